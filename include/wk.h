@@ -6,6 +6,8 @@
  *   - the chunk pool of evicted KV chunks (Section 4.2):  wk_pool_append / wk_pool_evict
  *   - World Retrieval (Section 4.2 Eq. 4, distance of Section 5.1): wk_retrieve
  *   - attention of the denoising chunk over [window + retrieved chunks] (Section 4.2): wk_memory_attention
+ * and, beside the chunk pool, a key/value cache in pages for programs that generate token by token (no counterpart in the
+ * paper): wk_page_plan, wk_page_store, wk_paged_attention
  *
  * Conventions
  *   - All tensor arguments are DEVICE pointers unless the name ends in _host.  bf16 tensors are
@@ -38,7 +40,7 @@ enum {
   WK_OK = 0,
   WK_ERR_ARG = -1,        /* NULL pointer, misaligned pointer, negative count, bad config field */
   WK_ERR_SHAPE = -2,      /* a size outside what the context was created for */
-  WK_ERR_POOL_FULL = -3,  /* wk_pool_append with no free slot */
+  WK_ERR_POOL_FULL = -3,  /* wk_pool_append with no free slot; reported by wk_poll_status: wk_page_plan refused a request */
   WK_ERR_BAD_SLOT = -4,   /* host-visible slot id out of range or not valid */
   WK_ERR_CUDA = -5,       /* a CUDA runtime/driver call failed (wk_last_cuda_error has the code) */
   WK_ERR_TIMEOUT = -6,    /* reported by wk_poll_status: a bounded device wait ran out */
@@ -48,7 +50,7 @@ enum {
 };
 
 /* bits of the device status word (wk_poll_status) */
-enum { WK_DEV_BAD_SLOT = 1u, WK_DEV_TIMEOUT = 2u, WK_DEV_NONFINITE = 4u };
+enum { WK_DEV_BAD_SLOT = 1u, WK_DEV_TIMEOUT = 2u, WK_DEV_NONFINITE = 4u, WK_DEV_POOL_FULL = 8u };
 
 typedef struct wk_ctx wk_ctx;
 
@@ -253,6 +255,94 @@ typedef struct {
 wk_status wk_memory_attention(wk_ctx* ctx, int32_t layer, const void* Q, int32_t lq, const wk_dense_seg* segs_host,
                               int32_t n_segs, const int32_t* slots_dev, int32_t n_slots, void* O, float* lse_out,
                               int32_t kv_splits, void* stream);
+
+/* ---- token-level cache in pages ------------------------------------------------------------- */
+
+/* The chunk pool stores whole chunks of one stream.  Programs that generate token by token, for many requests of any length
+ * each, keep their keys and values in pages instead: page_tokens tokens a page, any page for any request, a table per request
+ * that lists its pages in order.  One wk_paged_kv is one layer's cache; the layers of a model share tables and slots.
+ * These calls take device, SM count and status word from ctx and touch neither its pool nor its scratch; an unbound context
+ * is fine (it has no status word: anomalies that only the device sees then go unreported). */
+
+enum { WK_BF16 = 0, WK_F16 = 1, WK_E4M3 = 2 };
+
+typedef struct {
+  void* K;               /* [n_pages][page_tokens][n_kv_heads][head_dim], places given by the strides; 16-byte aligned */
+  void* V;               /* the same layout */
+  uint8_t* K_exp;        /* WK_E4M3: [n_pages][n_kv_heads][page_tokens], contiguous: a row stands for its codes times */
+  uint8_t* V_exp;        /*   2^(byte - 127), byte in 1 .. 254; otherwise NULL */
+  int64_t page_stride;   /* elements, multiples of 16 bytes, the rows of a cache not overlapping */
+  int64_t token_stride;
+  int64_t head_stride;
+  int32_t n_pages;       /* n_pages * page_tokens < 2^31 */
+  int32_t page_tokens;   /* >= 1 */
+  int32_t n_kv_heads;
+  int32_t head_dim;      /* 64 or 128 */
+  int32_t type;          /* WK_BF16, WK_F16 or WK_E4M3 */
+  int32_t reserved;      /* 0 */
+} wk_paged_kv;
+
+/* Hands out pages and slots for the tokens of the next step, on the GPU, from lengths that live there.  Request r holds
+ * lens[r] tokens and gets new_tokens[r] more; its pages are tables[r][0 .. ceil(lens[r] / page_tokens)).
+ *   new_tokens[r] > 0   takes ceil((lens + new) / page_tokens) - ceil(lens / page_tokens) pages off the front of the ring of
+ *                       free pages, in request order, and enters them in the table.  A request is refused, and keeps its length, if its
+ *                       table has no room, if its rows reach past max_tokens, or if the pages that it and all requests before it
+ *                       ask for are more than are free (one that needs no new page is not refused for that):
+ *                       WK_DEV_POOL_FULL is set
+ *   new_tokens[r] < 0   the request ends: its pages go to the back of the ring (for the next call), its length becomes 0; its
+ *                       table row stays as it is.  Entries outside 0 .. n_pages - 1 are left out (other than -1: WK_DEV_BAD_SLOT)
+ *   lens[r] < 0         no request: takes no part (with new_tokens[r] > 0 it is refused)
+ *   lens_out [n_req]    the lengths afterwards; may be lens
+ *   tables [n_req]      rows of max_pages int32, table_stride apart; only new entries are written
+ *   ring [n_pages]      page ids; the free ones are ring[(head + i) mod n_pages], i < count
+ *   state [4]           head, count, and two words that are zero before the first call (the kernel uses them and leaves
+ *                       them zero).  state_out [4] receives head and count afterwards and two zeros; may be state.  At most
+ *                       n_pages pages are ever free; a page that would be one too many is dropped, a head or count out of range counts as no
+ *                       free pages; both set WK_DEV_BAD_SLOT
+ *   slots_out [max_tokens]   slot (page * page_tokens + place in the page) of every new token, request after request; -1 for the
+ *                       rows of refused requests, for tokens whose page id is out of range (WK_DEV_BAD_SLOT), and past the last row
+ *   starts_out [n_req + 1]   first row of every request, then the number of rows (int32, saturating)
+ * Errors: WK_ERR_SHAPE (n_req > 4096, n_req * max_pages or n_pages * page_tokens >= 2^31), WK_ERR_ARG. */
+wk_status wk_page_plan(wk_ctx* ctx, int32_t n_pages, int32_t page_tokens, int32_t n_req, const int32_t* lens,
+                       const int32_t* new_tokens, int32_t* lens_out, int32_t* tables, int32_t max_pages,
+                       int64_t table_stride, int32_t* ring, int32_t* state, int32_t* state_out, int32_t max_tokens,
+                       int32_t* slots_out, int32_t* starts_out, void* stream);
+
+/* Writes rows of K and V into their slots.  A slot of -1 is skipped silently, any other one outside the cache is skipped and sets
+ * WK_DEV_BAD_SLOT; slots must be distinct (one given twice ends as a mixture).
+ *   K_new, V_new [n_tokens][n_kv_heads][head_dim] of src_type, rows row_stride elements apart (a multiple of 8), 16-byte
+ *             aligned; src_type is the cache's type, or WK_BF16 or WK_F16 for a cache in 8 bits
+ *   WK_E4M3: a row (one token, one head) is stored with the smallest exponent e in -126 .. 127 for which its largest finite
+ *             magnitude is at most 448 * 2^e (0 for a row of zeros), each value rounded to the nearest code, ties to even.
+ *             Values that are not finite become NaN and set WK_DEV_NONFINITE
+ * Errors: WK_ERR_ARG, WK_ERR_SHAPE. */
+wk_status wk_page_store(wk_ctx* ctx, const wk_paged_kv* cache, const void* K_new, const void* V_new, int32_t src_type,
+                        int32_t n_tokens, int64_t row_stride, const int32_t* slots, void* stream);
+
+/* Scratch of wk_paged_attention: partial results of requests that several CTAs share, and their counters.  Zero-filled by the
+ * caller the first time; every call leaves the counters zero.  Calls that share it must not overlap on the GPU. */
+size_t wk_paged_scratch_bytes(const wk_ctx* ctx);
+
+/* Attention of one new token per request: for request r and head h, with kv head h / (n_heads / n_kv_heads),
+ *   O[r][h] = sum_t softmax_t(scale * Q[r][h] . K_t) V_t   over the request's first lens[r] tokens (the new one among them),
+ * or, with window > 0, over its first `sink` and its last `window` tokens.  The lengths are read on the GPU: a captured call follows
+ * them.  The work is cut into equal shares of all requests' tokens, whatever their lengths, and joined in a fixed order.
+ *   Q [n_req][n_heads][head_dim] of q_type, rows q_stride elements apart (a multiple of 8); O the same, contiguous; O may be Q
+ *             where that is contiguous too.  q_type is the cache's type, or WK_BF16 or WK_F16 for a cache in 8 bits
+ *   tables [n_req] rows of max_pages int32, table_stride apart.  The tokens of a page listed as -1 are skipped silently, those of
+ *             any other id out of range are skipped and set WK_DEV_BAD_SLOT; a length beyond the table counts as the table's
+ *             (WK_DEV_BAD_SLOT)
+ *   lens [n_req]  0: nothing is attended, O = 0 and lse = -inf; negative: the request's rows of O and lse_out stay as they are
+ *   lse_out [n_req][n_heads] fp32 (natural log) or NULL.  A row in which no key has any weight (none visible, all logits
+ *             -inf) is O = 0, lse = -inf; a logit that is NaN or +inf makes its row NaN
+ *   softmax_scale 0 selects 1/sqrt(head_dim); window 0: all tokens
+ *   scratch   wk_paged_scratch_bytes() bytes, 256-byte aligned
+ * Errors: WK_ERR_SHAPE (n_heads not a multiple of n_kv_heads, scratch too small, a cache of 64 GB or more), WK_ERR_ARG. */
+wk_status wk_paged_attention(wk_ctx* ctx, const wk_paged_kv* cache, const void* Q, int32_t q_type, int64_t q_stride,
+                             int32_t n_req, int32_t n_heads, const int32_t* tables, int32_t max_pages,
+                             int64_t table_stride, const int32_t* lens, int32_t window, int32_t sink,
+                             float softmax_scale, void* O, float* lse_out, void* scratch, size_t scratch_bytes,
+                             void* stream);
 
 /* ---- status -------------------------------------------------------------------------------- */
 

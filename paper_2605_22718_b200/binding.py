@@ -18,7 +18,7 @@ LIB_PATH = os.path.join(_HERE, "libworldkv.so")
 WK_OK = 0
 WK_ERR_ARG, WK_ERR_SHAPE, WK_ERR_POOL_FULL, WK_ERR_BAD_SLOT = -1, -2, -3, -4
 WK_ERR_CUDA, WK_ERR_TIMEOUT, WK_ERR_NONFINITE, WK_ERR_UNBOUND, WK_ERR_NO_DEVICE = -5, -6, -7, -8, -9
-WK_DEV_BAD_SLOT, WK_DEV_TIMEOUT, WK_DEV_NONFINITE = 1, 2, 4
+WK_DEV_BAD_SLOT, WK_DEV_TIMEOUT, WK_DEV_NONFINITE, WK_DEV_POOL_FULL = 1, 2, 4, 8
 
 
 class wk_config(C.Structure):
@@ -32,7 +32,16 @@ class wk_dense_seg(C.Structure):
     _fields_ = [("K", C.c_void_p), ("V", C.c_void_p), ("n_tokens", C.c_int32), ("reserved", C.c_int32)]
 
 
+class wk_paged_kv(C.Structure):
+    _fields_ = [("K", C.c_void_p), ("V", C.c_void_p), ("K_exp", C.c_void_p), ("V_exp", C.c_void_p),
+                ("page_stride", C.c_int64), ("token_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("n_pages", C.c_int32), ("page_tokens", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("type", C.c_int32), ("reserved", C.c_int32)]
+
+
 SCORE_WHOLE_KEY, SCORE_PER_HEAD = 0, 2     # wk_config.score_mode
+WK_BF16, WK_F16, WK_E4M3 = 0, 1, 2         # wk_paged_kv.type
+_TYPES = {torch.bfloat16: WK_BF16, torch.float16: WK_F16, torch.float8_e4m3fn: WK_E4M3}
 
 
 class WkError(RuntimeError):
@@ -78,6 +87,11 @@ def load_library() -> C.CDLL:
         "wk_retrieve_scan": (i32, [vp, vp, vp, C.c_int64, C.POINTER(C.c_float), i32, vp, vp, i32, vp, C.c_size_t, vp]),
         "wk_retrieve_noalloc": (i32, [vp, vp, i32, C.POINTER(C.c_float), i32, i32, vp, vp, vp]),
         "wk_memory_attention": (i32, [vp, i32, vp, i32, C.POINTER(wk_dense_seg), i32, vp, i32, vp, vp, i32, vp]),
+        "wk_page_plan": (i32, [vp, i32, i32, i32, vp, vp, vp, vp, i32, i64, vp, vp, vp, i32, vp, vp, vp]),
+        "wk_page_store": (i32, [vp, vp, vp, vp, i32, i32, i64, vp, vp]),
+        "wk_paged_scratch_bytes": (sz, [vp]),
+        "wk_paged_attention": (i32, [vp, vp, vp, i32, i64, i32, i32, vp, i32, i64, vp, i32, i32, C.c_float, vp, vp, vp, sz,
+                                     vp]),
         "wk_poll_status": (i32, [vp, C.POINTER(C.c_uint32), vp]),
         "wk_status_string": (C.c_char_p, [i32]),
         "wk_last_cuda_error": (i32, [vp]),
@@ -95,7 +109,8 @@ EXPORTED_SYMBOLS = ("wk_create", "wk_destroy", "wk_pool_bytes", "wk_scratch_byte
                     "wk_pool_append", "wk_pool_compress_append", "wk_pool_evict", "wk_pool_oldest", "wk_pool_count", "wk_pool_tag", "wk_retrieve",
                     "wk_retrieve_noalloc", "wk_retrieve_query", "wk_retrieve_scan", "wk_retrieve_scan_scratch_bytes",
                     "wk_host_chunk_bytes", "wk_pool_store_host", "wk_pool_load_host",
-                    "wk_memory_attention", "wk_poll_status", "wk_status_string", "wk_last_cuda_error",
+                    "wk_memory_attention", "wk_page_plan", "wk_page_store", "wk_paged_scratch_bytes", "wk_paged_attention",
+                    "wk_poll_status", "wk_status_string", "wk_last_cuda_error",
                     "wk_launch_count")
 
 
@@ -342,3 +357,148 @@ class WorldKV:
 
     def last_cuda_error(self) -> int:
         return self.lib.wk_last_cuda_error(self.ctx)
+
+
+class PagedKV:
+    """One layer's token-level cache in pages, on the device of a WorldKV context.
+
+    K, V: [n_pages, page_tokens, n_kv_heads, head_dim] CUDA tensors of bf16, fp16 or float8_e4m3fn, head_dim 64 or 128, any
+    strides that are multiples of 16 bytes (last axis contiguous; K and V alike).  In 8 bits K_exp and V_exp are uint8
+    [n_pages, n_kv_heads, page_tokens], contiguous.  ``PagedKV.empty`` allocates them.  A cache made from n_pages and
+    page_tokens alone only plans.  Method names and arguments mirror include/wk.h.
+    """
+
+    def __init__(self, kv: WorldKV, K: Optional[torch.Tensor] = None, V: Optional[torch.Tensor] = None,
+                 K_exp: Optional[torch.Tensor] = None, V_exp: Optional[torch.Tensor] = None,
+                 n_pages: Optional[int] = None, page_tokens: Optional[int] = None):
+        self.kv, self.lib, self.device = kv, kv.lib, kv.device
+        self._index = kv.device.index
+        self.K, self.V, self.K_exp, self.V_exp = K, V, K_exp, V_exp
+        self._desc = None
+        if K is None:
+            _need(n_pages is not None and page_tokens is not None, "PagedKV: K and V, or n_pages and page_tokens")
+            self.n_pages, self.page_tokens = n_pages, page_tokens
+            return
+        _need(V is not None and K.dim() == 4 and K.shape == V.shape and K.stride() == V.stride() and K.dtype == V.dtype
+              and K.dtype in _TYPES and K.stride(3) == 1, "PagedKV: K and V of one shape, type and layout")
+        self.n_pages, self.page_tokens, self.n_kv_heads, self.head_dim = K.shape
+        self.type = _TYPES[K.dtype]
+        self._on_device("PagedKV", K, V, K_exp, V_exp)
+        if self.type == WK_E4M3:
+            for e in (K_exp, V_exp):
+                _need(e is not None and e.dtype == torch.uint8 and e.is_contiguous()
+                      and e.shape == (self.n_pages, self.n_kv_heads, self.page_tokens), "PagedKV: K_exp and V_exp")
+        else:
+            _need(K_exp is None and V_exp is None, "PagedKV: exponents belong to a cache in 8 bits")
+        self._desc = wk_paged_kv(K.data_ptr(), V.data_ptr(), _ptr(K_exp), _ptr(V_exp), K.stride(0), K.stride(1), K.stride(2),
+                                 self.n_pages, self.page_tokens, self.n_kv_heads, self.head_dim, self.type, 0)
+        self._desc_at = C.addressof(self._desc)
+        if getattr(kv, "paged_scratch", None) is None:     # shared by the caches of a context, like its other scratch
+            kv.paged_scratch = torch.zeros(self.lib.wk_paged_scratch_bytes(kv.ctx), dtype=torch.uint8, device=self.device)
+            torch.cuda.synchronize(self.device)
+
+    @classmethod
+    def empty(cls, kv: WorldKV, n_pages: int, page_tokens: int, n_kv_heads: int, head_dim: int = 128,
+              dtype: torch.dtype = torch.bfloat16) -> "PagedKV":
+        shape = (n_pages, page_tokens, n_kv_heads, head_dim)
+        pages = [torch.empty(shape, dtype=dtype, device=kv.device) for _ in range(2)]
+        exps = [torch.full((n_pages, n_kv_heads, page_tokens), 127, dtype=torch.uint8, device=kv.device)
+                if dtype == torch.float8_e4m3fn else None for _ in range(2)]
+        return cls(kv, *pages, *exps)
+
+    def _on_device(self, what: str, *tensors) -> None:
+        for x in tensors:
+            _need(x is None or (x.is_cuda and x.get_device() == self._index), what + ": tensors on the context's device")
+
+    def _stream(self, stream) -> int:
+        return stream.cuda_stream if stream else torch._C._cuda_getCurrentRawStream(self._index)
+
+    def free_pages(self) -> Tuple[torch.Tensor, torch.Tensor]:
+        """(ring, state) for page_plan with every page free."""
+        ring = torch.arange(self.n_pages, dtype=torch.int32, device=self.device)
+        return ring, torch.tensor([0, self.n_pages, 0, 0], dtype=torch.int32, device=self.device)
+
+    def page_plan(self, lens: torch.Tensor, new_tokens: torch.Tensor, tables: torch.Tensor, ring: torch.Tensor,
+                  state: torch.Tensor, max_tokens: int, lens_out: Optional[torch.Tensor] = None,
+                  state_out: Optional[torch.Tensor] = None, slots_out: Optional[torch.Tensor] = None,
+                  starts_out: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """Pages and slots for the next step's tokens; lens and state are advanced in place unless lens_out, state_out are
+        given.  Returns (slots [max_tokens], starts [n_req + 1]) int32, on the device."""
+        n = lens.size(0)
+        lens_out = lens if lens_out is None else lens_out
+        state_out = state if state_out is None else state_out
+        if slots_out is None:
+            slots_out = torch.empty(max_tokens, dtype=torch.int32, device=self.device)
+        if starts_out is None:
+            starts_out = torch.empty(n + 1, dtype=torch.int32, device=self.device)
+        for x, size in ((lens, n), (new_tokens, n), (lens_out, n), (ring, self.n_pages), (state, 4), (state_out, 4),
+                        (slots_out, max_tokens), (starts_out, n + 1)):
+            _need(x.dtype == torch.int32 and x.dim() == 1 and x.size(0) >= size and x.is_contiguous()
+                  and x.get_device() == self._index, "wk_page_plan: int32 arrays of the right length on the context's device")
+        _need(tables.dtype == torch.int32 and tables.dim() == 2 and tables.size(0) >= n and tables.stride(1) == 1
+              and tables.get_device() == self._index, "wk_page_plan: tables [n_req, max_pages] int32")
+        st = self.lib.wk_page_plan(self.kv.ctx, self.n_pages, self.page_tokens, n, lens.data_ptr(), new_tokens.data_ptr(),
+                                   lens_out.data_ptr(), tables.data_ptr(), tables.size(1), tables.stride(0), ring.data_ptr(),
+                                   state.data_ptr(), state_out.data_ptr(), max_tokens, slots_out.data_ptr(),
+                                   starts_out.data_ptr(), self._stream(stream))
+        if st != WK_OK:
+            raise WkError(st, "wk_page_plan")
+        return slots_out, starts_out
+
+    def page_store(self, K_new: torch.Tensor, V_new: torch.Tensor, slots: torch.Tensor, stream=None) -> None:
+        """Rows K_new, V_new [n, n_kv_heads, head_dim] (heads contiguous, any row stride, both alike) into slots [>= n]."""
+        n = K_new.size(0)
+        row = (self.n_kv_heads, self.head_dim)
+        _need(self._desc is not None and K_new.shape == V_new.shape and K_new.shape[1:] == row and K_new.dtype == V_new.dtype
+              and K_new.dtype in _TYPES and K_new.stride() == V_new.stride() and _rows(K_new) and K_new.get_device() == self._index
+              and V_new.get_device() == self._index,
+              "wk_page_store: K_new, V_new [n, n_kv_heads, head_dim] alike, heads contiguous")
+        _need(slots.dtype == torch.int32 and slots.dim() == 1 and slots.size(0) >= n and slots.is_contiguous()
+              and slots.get_device() == self._index, "wk_page_store: slots int32")
+        st = self.lib.wk_page_store(self.kv.ctx, self._desc_at, K_new.data_ptr(), V_new.data_ptr(), _TYPES[K_new.dtype], n,
+                                    K_new.stride(0), slots.data_ptr(), self._stream(stream))
+        if st != WK_OK:
+            raise WkError(st, "wk_page_store")
+
+    def paged_attention(self, Q: torch.Tensor, tables: torch.Tensor, lens: torch.Tensor, window: int = 0, sink: int = 0,
+                        softmax_scale: float = 0.0, O: Optional[torch.Tensor] = None, lse_out: Optional[torch.Tensor] = None,
+                        scratch: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+        """O [n_req, n_heads, head_dim] of one new token per request: Q [n_req, n_heads, head_dim] (heads contiguous, any
+        row stride) over the tokens that tables and lens name.  scratch: as WorldKV's, shared by the calls of a context unless
+        given (zero-filled once; for calls that may overlap on the GPU)."""
+        n, heads, d = Q.shape
+        if scratch is None:
+            scratch = self.kv.paged_scratch
+        _need(self._desc is not None and d == self.head_dim and Q.dtype in _TYPES and _rows(Q) and Q.get_device() == self._index,
+              "wk_paged_attention: Q [n_req, n_heads, head_dim], heads contiguous")
+        _need(tables.dtype == torch.int32 and tables.dim() == 2 and tables.size(0) >= n and tables.stride(1) == 1
+              and tables.get_device() == self._index and lens.dtype == torch.int32 and lens.dim() == 1 and lens.size(0) >= n
+              and lens.is_contiguous() and lens.get_device() == self._index,
+              "wk_paged_attention: tables [n_req, max_pages] and lens [n_req] int32")
+        if O is None:
+            O = torch.empty((n, heads, d), dtype=Q.dtype, device=self.device)
+        else:
+            _need(O.shape == Q.shape and O.dtype == Q.dtype and O.is_contiguous() and O.get_device() == self._index,
+                  "wk_paged_attention: O like Q, contiguous")
+        if lse_out is not None:
+            _need(lse_out.shape == (n, heads) and lse_out.dtype == torch.float32 and lse_out.is_contiguous()
+                  and lse_out.get_device() == self._index, "wk_paged_attention: lse_out [n_req, n_heads] fp32")
+        if n == 0:
+            return O
+        st = self.lib.wk_paged_attention(self.kv.ctx, self._desc_at, Q.data_ptr(), _TYPES[Q.dtype], Q.stride(0), n, heads,
+                                         tables.data_ptr(), tables.size(1), tables.stride(0), lens.data_ptr(), window, sink,
+                                         softmax_scale, O.data_ptr(), _ptr(lse_out), scratch.data_ptr(), scratch.numel(),
+                                         self._stream(stream))
+        if st != WK_OK:
+            raise WkError(st, f"wk_paged_attention (last CUDA error {self.kv.last_cuda_error()})")
+        return O
+
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise WkError(WK_ERR_ARG, what)
+
+
+def _rows(x: torch.Tensor) -> bool:
+    """Rows [n, heads, head_dim] whose heads lie one after the other."""
+    return x.stride(2) == 1 and (x.size(1) == 1 or x.stride(1) == x.size(2))

@@ -126,8 +126,6 @@ const CUtensorMap* cached_rows_map(wk_ctx* ctx, const void* base, int32_t rows, 
   return &ctx->tmap_cache[i].map;
 }
 
-static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
 static wk_status check_config(const wk_config* c) {
   if (!c) return WK_ERR_ARG;
   if (c->head_dim != kHeadDim) return WK_ERR_ARG;
@@ -140,19 +138,6 @@ static wk_status check_config(const wk_config* c) {
   if (static_cast<int64_t>(c->n_layers) * c->pool_slots > 0x7fffffffLL) return WK_ERR_ARG;
   return WK_OK;
 }
-
-// Every entry point that touches the device runs on the context's own device, whatever the caller had current.
-static wk_status use_device(wk_ctx* ctx) {
-  int dev = -1;
-  WK_CUDA_TRY(ctx, cudaGetDevice(&dev));
-  if (dev != ctx->cfg.device) WK_CUDA_TRY(ctx, cudaSetDevice(ctx->cfg.device));
-  return WK_OK;
-}
-#define WK_USE_DEVICE(ctx)                                  \
-  do {                                                      \
-    wk_status st__ = ::wk::use_device(ctx);                 \
-    if (st__ != WK_OK) return st__;                         \
-  } while (0)
 
 }  // namespace wk
 
@@ -534,6 +519,7 @@ wk_status wk_poll_status(wk_ctx* ctx, uint32_t* device_flags, void* stream) {
   if (flags & WK_DEV_TIMEOUT) return WK_ERR_TIMEOUT;
   if (flags & WK_DEV_NONFINITE) return WK_ERR_NONFINITE;
   if (flags & WK_DEV_BAD_SLOT) return WK_ERR_BAD_SLOT;
+  if (flags & WK_DEV_POOL_FULL) return WK_ERR_POOL_FULL;
   return WK_OK;
 }
 

@@ -100,6 +100,21 @@ inline wk_status cuda_fail(wk_ctx* ctx, cudaError_t e) {
     if (e__ != cudaSuccess) return ::wk::cuda_fail(ctx, e__);  \
   } while (0)
 
+// Every entry point that touches the device runs on the context's own device, whatever the caller had current.
+inline wk_status use_device(wk_ctx* ctx) {
+  int dev = -1;
+  WK_CUDA_TRY(ctx, cudaGetDevice(&dev));
+  if (dev != ctx->cfg.device) WK_CUDA_TRY(ctx, cudaSetDevice(ctx->cfg.device));
+  return WK_OK;
+}
+#define WK_USE_DEVICE(ctx)                                  \
+  do {                                                      \
+    wk_status st__ = ::wk::use_device(ctx);                 \
+    if (st__ != WK_OK) return st__;                         \
+  } while (0)
+
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
 inline wk_status after_launch(wk_ctx* ctx, int n = 1) {
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess) return cuda_fail(ctx, e);
@@ -187,5 +202,40 @@ wk_status launch_attention(wk_ctx* ctx, int layer, const __nv_bfloat16* Q, int l
                            cudaStream_t s, bool lse_only = false);
 wk_status launch_retrieve_query(wk_ctx* ctx, int layer, const __nv_bfloat16* Q, int lq, int k, int32_t* slots_out,
                                 float* score_out, cudaStream_t s);
+
+// Token-level cache in pages (entry points in wk_paged_api.cu).
+constexpr int kPlanMaxReq = 4096;
+struct PlanArgs {
+  int32_t n_pages, page_tokens, n_req;
+  const int32_t *lens, *more;
+  int32_t *lens_out, *tables;
+  int32_t max_pages;
+  int64_t table_stride;
+  int32_t *ring, *state, *state_out;
+  int32_t max_tokens;
+  int32_t *slots, *starts;
+  uint32_t* status;             // null: the context is not bound
+};
+wk_status launch_page_plan(wk_ctx* ctx, const PlanArgs& a, cudaStream_t s);
+wk_status launch_page_store(wk_ctx* ctx, const wk_paged_kv& c, const void* K_new, const void* V_new, int src_type, int n_tokens,
+                            int64_t row_stride, const int32_t* slots, cudaStream_t s);
+struct PagedArgs {
+  wk_paged_kv c;
+  const void* Q;
+  int64_t q_stride;
+  int32_t q_type, n_req, n_heads;
+  const int32_t* tables;
+  int32_t max_pages;
+  int64_t table_stride;
+  const int32_t* lens;
+  int32_t window, sink;         // window 0: all tokens are visible
+  float scale;
+  void* O;
+  float* lse;
+  uint8_t* scratch;
+  uint32_t* status;
+};
+wk_status launch_paged_attention(wk_ctx* ctx, const PagedArgs& a, cudaStream_t s);
+size_t paged_scratch_bytes(int sm_count);
 
 }  // namespace wk
