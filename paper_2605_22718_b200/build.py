@@ -20,7 +20,7 @@ LIB_INPUTS = os.path.join(ROOT, "wkinputs", "libwkinputs.so")
 LIB_WAIT_PROBE = os.path.join(ROOT, "tests", "cuda", "libwk_wait_probe.so")
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-shared",
-              "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
+              "-Xcompiler", "-fPIC", "-Xptxas", "-v", "--threads", "0"]
 
 
 def _nvcc() -> str:
