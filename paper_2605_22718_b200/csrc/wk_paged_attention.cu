@@ -5,15 +5,16 @@
 // flight.
 //
 //   * Work.  A unit is (request, kv head, up to 8 * NT of the query heads that share it).  A unit's tokens are cut into steps of ST
-//     tokens; all steps of all units form one line, and every CTA takes an equal run of it (one CTA per SM), every warp an equal
-//     run of the CTA's.  So lengths of any spread load all SMs alike, the grid does not depend on the lengths (a captured call
-//     follows them), and a unit is cut only where a run ends.  The lengths are summed by every CTA for itself.
-//   * A warp walks its run alone: no barrier, no shared memory.  K and V go from global memory to registers in the places where the
-//     matrix instructions want them: S^T = K Q^T has tokens as rows, so a lane's 16 contiguous bytes of a key are four (bf16, fp16)
-//     or sixteen (8 bits) places along the contracted axis, whose order is free as long as Q is laid out alike; O^T = V^T P^T
-//     has the head's dimensions as rows, so a lane's 16 bytes of two tokens are paired up by byte permutes.  P^T comes from S^T
-//     by an 8x8 transpose in the registers of the warp.  The next step's K is loaded as soon as S is done, its V as soon as O
-//     is, and the page ids of the step after that are looked up meanwhile.
+//     tokens (8 KB of K and V); all steps of all units form one line, and every CTA takes an equal run of it (one CTA per SM),
+//     every warp an equal run of the CTA's.  So lengths of any spread load all SMs alike, the grid does not depend on the lengths
+//     (a captured call follows them), and a unit is cut only where a run ends.  The lengths are summed by every CTA for itself.
+//   * A warp walks its run alone, without barriers: it copies the rows of coming steps into its own ring in shared memory
+//     (16-byte asynchronous copies, tokens that are not attended become zeros) and multiplies out of it.  Page ids are looked up
+//     a step before their rows are asked for.
+//   * S^T = K Q^T and O^T = V^T P^T: tokens, then dimensions are the rows of the 16 x 8 x 16 matrix instructions, query heads their
+//     columns.  (With one token per request there are at most a few columns: the instructions of the SM's large matrix unit
+//     work on 64 rows at least and would be filled no better, and the time goes into the copies.)  P^T comes from S^T by an
+//     8 x 8 transpose in the warp's registers.
 //   * Softmax.  Per query head a reference close to the running maximum: it moves only when a logit exceeds it by more than 8 (in
 //     log2), which one vote per step finds out, so weights reach at most 2^8; sums are fp32.  Weights are rounded to the type of V
 //     for the second product (bf16 or fp16, half a step 2^-8 or 2^-11 of the weight; the normalising sum is of the unrounded ones).
@@ -24,6 +25,7 @@
 //     scratch buffer; the CTA that arrives last joins them in their order, so that the result does not depend on the arrival.
 #include <cuda_fp16.h>
 
+#include "ptx_sm100.cuh"
 #include "wk_internal.cuh"
 
 namespace wk {
@@ -31,7 +33,9 @@ namespace {
 
 constexpr uint32_t kNowhere = 0xffffffffu;   // row offset of a token that is not attended
 constexpr float kLazy = 8.f;                 // how far (log2) a logit may exceed the reference
-constexpr float kLn2 = 0.6931471805599453f;
+constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
+constexpr int kStepBytes = 8192;             // of K and V in a step
+constexpr int kMaxWarps = 12;
 
 struct Params {
   PagedArgs a;
@@ -46,31 +50,31 @@ template <int MODE, int D, int NT>
 struct Shape {
   static constexpr int ES = MODE == WK_E4M3 ? 1 : 2;     // bytes per element of the cache
   static constexpr int ROW = D * ES;                     // bytes of a row
-  static constexpr int TT = 256 / ROW;                   // tiles of 16 tokens in a step: K and V of a step are 8 KB
-  static constexpr int ST = 16 * TT;
+  static constexpr int ST = kStepBytes / 2 / ROW;        // tokens of a step: 16, 32 or 64
   static constexpr int RL = ST > 32 ? ST / 32 : 1;       // tokens per lane when rows are looked up
-  static constexpr int KV = ROW / 64;                    // 16-byte loads of a key per lane (four lanes read 64 bytes)
-  static constexpr int VH = ROW / 128 > 0 ? ROW / 128 : 1, VR = ROW / 128 > 0 ? 4 : 2;   // loads of a value per lane, registers each
-  static constexpr int W = NT == 1 ? 12 : 8;             // warps: what the registers of an SM hold
+  static constexpr int LPR = ROW / 16;                   // lanes (16-byte chunks) per row
+  static constexpr int RPI = 32 / LPR;                   // rows per copy instruction
   static constexpr int PADDED = D + 4;
-  static constexpr int SMEM = 2 * W * 8 * NT * PADDED * 4;
+  static constexpr int PIECE = 8 * NT * PADDED * 4;      // bytes of a piece in shared memory
+  static constexpr int META = MODE == WK_E4M3 ? 2 * ST : 0;   // exponents of a step's tokens
 };
 
 // ---------------------------------------------------------------- instructions
-__device__ __forceinline__ void load16(uint32_t (&r)[4], const void* p, bool on) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %5, 0;\n\t"
-      "mov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\tmov.b32 %2, 0;\n\tmov.b32 %3, 0;\n\t"
-      "@p ld.global.nc.L1::no_allocate.v4.b32 {%0, %1, %2, %3}, [%4];\n\t}"
-      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
-      : "l"(p), "r"(static_cast<uint32_t>(on)));
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint32_t skip) {   // zeros, and nothing read, where skip is not 0
+  asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\tcp.async.cg.shared.global [%0], [%1], 16, p;\n\t}"
+               ::"r"(dst), "l"(src), "r"(skip) : "memory");
 }
-__device__ __forceinline__ void load8(uint32_t (&r)[2], const void* p, bool on) {
-  asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %3, 0;\n\tmov.b32 %0, 0;\n\tmov.b32 %1, 0;\n\t"
-      "@p ld.global.nc.L1::no_allocate.v2.b32 {%0, %1}, [%2];\n\t}"
-      : "=r"(r[0]), "=r"(r[1])
-      : "l"(p), "r"(static_cast<uint32_t>(on)));
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+template <bool TRANS>
+__device__ __forceinline__ void load_matrices(uint32_t (&r)[4], uint32_t addr) {
+  if (TRANS)
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+  else
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
 // d += a b on a 16 x 8 x 16 tile
 template <bool BF16>
@@ -94,11 +98,6 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
   else asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
 }
-__device__ __forceinline__ float exp2_of(float x) {
-  float y;
-  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-  return y;
-}
 // two codes to two fp16, exactly
 __device__ __forceinline__ uint32_t codes_lo(uint32_t w) {
   uint32_t r;
@@ -116,6 +115,7 @@ __device__ __forceinline__ float lo_of(uint32_t w, bool bf16) {
 __device__ __forceinline__ float hi_of(uint32_t w, bool bf16) {
   return bf16 ? __uint_as_float(w & 0xffff0000u) : __half2float(__ushort_as_half(static_cast<uint16_t>(w >> 16)));
 }
+using ptx::ex2_approx;
 
 // ---------------------------------------------------------------- units
 struct Unit {
@@ -135,27 +135,33 @@ __device__ __forceinline__ int32_t measure(const Params& p, int r, int32_t* show
   return *shown > ST ? static_cast<int32_t>((static_cast<uint32_t>(*shown) + ST - 1) / ST) : 1;
 }
 
+// a / b of numbers that hardly ever need 64 bits.  (One copy of the long way: a CTA runs most of this kernel's code once, and
+// fetching instructions is then a good part of what that costs.)
+__device__ __noinline__ int64_t quotient64(int64_t a, int64_t b) { return a / b; }
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+  return (a | b) >> 32 ? quotient64(a, b) : static_cast<int64_t>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b));
+}
+
 // The unit that place x of the line lies in.  pre[t]: steps of one unit of each request before thread t's `per` requests.
-template <int ST, int THREADS>
+template <int ST>
 __device__ __forceinline__ Unit locate(const Params& p, const int64_t* pre, int per, int64_t x) {
-  const int64_t z = x / p.units;
-  int lo = 0, hi = THREADS;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (pre[mid] <= z) lo = mid; else hi = mid;
-  }
+  const int64_t z = quotient(x, p.units);
+  int lo = -1;   // (the whole warp is here)
+#pragma unroll 4
+  for (int k = 0; k < blockDim.x; k += 32) lo += __popc(__ballot_sync(0xffffffffu, pre[k + (threadIdx.x & 31)] <= z));
   Unit v;
   int64_t before = pre[lo];
   v.r = lo * per;
   v.shown = v.shift = 0;
   v.cost = measure<ST>(p, v.r, &v.shown, &v.shift);
+#pragma unroll 1
   while (before + v.cost <= z && v.r < p.a.n_req - 1) {   // (z lies before the sum of all: the second bound is for lengths that change meanwhile)
     before += v.cost;
     v.cost = measure<ST>(p, ++v.r, &v.shown, &v.shift);
   }
   v.cost = max(v.cost, 1);
   const int64_t rest = x - before * p.units;
-  v.u = static_cast<int32_t>(rest / v.cost);
+  v.u = static_cast<int32_t>(quotient(rest, v.cost));
   v.step = static_cast<int32_t>(rest - static_cast<int64_t>(v.u) * v.cost);
   return v;
 }
@@ -166,6 +172,7 @@ __device__ __forceinline__ void advance(const Params& p, Unit& v) {
   v.step = 0;
   if (++v.u < p.units) return;
   v.u = 0;
+#pragma unroll 1
   do v.cost = v.r < p.a.n_req - 1 ? measure<ST>(p, ++v.r, &v.shown, &v.shift) : 1;
   while (v.cost == 0);
 }
@@ -188,34 +195,76 @@ struct Piece {
   int32_t r, u, cost;   // r < 0: none
   int64_t start;        // the unit's first place in the line
 };
-
 constexpr int kPieceFloats = 16 * (128 + 1);   // of a piece in the scratch buffer: log-sum-exps, then rows
 constexpr size_t counter_bytes(int ctas) { return (ctas * sizeof(uint32_t) + 255) / 256 * 256; }
 
-template <bool QBF>
-__device__ __forceinline__ void store4(void* O, int64_t i, float4 v) {
-  *reinterpret_cast<uint2*>(static_cast<uint16_t*>(O) + i) = make_uint2(pack2<QBF>(v.x, v.y), pack2<QBF>(v.z, v.w));
+// A row of D values over the lanes of a warp.
+template <int D>
+struct Lane;
+template <>
+struct Lane<128> {
+  using Vec = float4;
+  static __device__ __forceinline__ void scale(Vec& v, float f) { v.x *= f; v.y *= f; v.z *= f; v.w *= f; }
+  static __device__ __forceinline__ void add(Vec& v, float e, const Vec& b) { v.x += e * b.x; v.y += e * b.y; v.z += e * b.z; v.w += e * b.w; }
+  template <bool BF16>
+  static __device__ __forceinline__ void store(void* O, int64_t i, int lane, const Vec& v) {
+    reinterpret_cast<uint2*>(static_cast<uint16_t*>(O) + i)[lane] = make_uint2(pack2<BF16>(v.x, v.y), pack2<BF16>(v.z, v.w));
+  }
+};
+template <>
+struct Lane<64> {
+  using Vec = float2;
+  static __device__ __forceinline__ void scale(Vec& v, float f) { v.x *= f; v.y *= f; }
+  static __device__ __forceinline__ void add(Vec& v, float e, const Vec& b) { v.x += e * b.x; v.y += e * b.y; }
+  template <bool BF16>
+  static __device__ __forceinline__ void store(void* O, int64_t i, int lane, const Vec& v) {
+    reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(O) + i)[lane] = pack2<BF16>(v.x, v.y);
+  }
+};
+// The share of the whole that each lane's log-sum-exp (log2) stands for; lse becomes that of the whole.
+__device__ __forceinline__ float join_weight(float& lse) {
+  float m = lse;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+  if (m == -INFINITY) m = 0.f;
+  const float e = ex2_approx(lse - m);
+  float l = e;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
+  lse = l == 0.f ? -INFINITY : m + __log2f(l);
+  return l == 0.f ? 0.f : __fdividef(e, l);
 }
 
 // ---------------------------------------------------------------- the kernel
-template <int MODE, int D, int NT, bool QBF>
-__global__ void __launch_bounds__(32 * Shape<MODE, D, NT>::W, 1)
+// Shared memory: a ring of STAGES steps per warp (at a warp's end also its last piece), the warps' first pieces, the steps' masks
+// and exponents.
+template <int MODE, int D, int NT, bool QBF, int STAGES>
+__global__ void __launch_bounds__(32 * kMaxWarps, 1)
 paged_attention(const __grid_constant__ Params p) {
   using S = Shape<MODE, D, NT>;
-  constexpr int ST = S::ST, TT = S::TT, W = S::W, THREADS = 32 * W, PADDED = S::PADDED;
+  constexpr int ST = S::ST, PADDED = S::PADDED, ROW = S::ROW;
   constexpr bool E4 = MODE == WK_E4M3, BF = MODE == WK_BF16;
-  constexpr int MT = D / 16;   // row tiles of O^T
-  extern __shared__ float4 dyn[];
-  float* const po = reinterpret_cast<float*>(dyn);          // [2 W][8 NT][PADDED]
-  __shared__ int64_t pre[THREADS], parts[W];
-  __shared__ float plse[2 * W][8 * NT];
-  __shared__ Piece piece[2 * W], split[2];
-  __shared__ int32_t last[2];
+  constexpr int MT = D / 16;   // row tiles of O^T, and steps along the dimensions in S
+  extern __shared__ __align__(1024) uint8_t dyn[];
+  __shared__ int64_t pre[32 * kMaxWarps], parts[kMaxWarps];
+  __shared__ float plse[2 * kMaxWarps][8 * NT];
+  __shared__ Piece piece[2 * kMaxWarps], split[2];
+  __shared__ uint32_t masks[kMaxWarps][STAGES][S::RL];
+  __shared__ int32_t first[2], count[2], n_groups, group_at[2 * kMaxWarps + 1];
+  const int W = blockDim.x >> 5, THREADS = blockDim.x;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
+  uint8_t* const ring = dyn + warp * (STAGES * kStepBytes);
+  uint8_t* const firsts = dyn + W * (STAGES * kStepBytes);
+  uint16_t* const exps = reinterpret_cast<uint16_t*>(firsts + W * S::PIECE) + warp * (STAGES * ST);
+  // piece i of the CTA (warp i / 2's first or last)
+  auto piece_rows = [&](int i) -> float* {
+    return reinterpret_cast<float*>(i & 1 ? dyn + (i >> 1) * (STAGES * kStepBytes) : firsts + (i >> 1) * S::PIECE);
+  };
 
   // ---- the line of steps, and this CTA's and this warp's run of it
   const int per = (p.a.n_req + THREADS - 1) / THREADS;
   int64_t mine = 0;
+#pragma unroll 1
   for (int i = 0; i < per; ++i) {
     const int r = tid * per + i;
     int32_t shown, shift;
@@ -232,7 +281,7 @@ paged_attention(const __grid_constant__ Params p) {
   if (lane == 31) parts[warp] = up;
   __syncthreads();
   int64_t before = 0, all = 0;
-#pragma unroll
+#pragma unroll 4
   for (int w = 0; w < W; ++w) {
     if (w < warp) before += parts[w];
     all += parts[w];
@@ -240,301 +289,271 @@ paged_attention(const __grid_constant__ Params p) {
   pre[tid] = before + up - mine;
   __syncthreads();
   const int64_t total = all * p.units;
-  int64_t chunk = (total + gridDim.x - 1) / gridDim.x;
+  int64_t chunk = quotient(total + gridDim.x - 1, gridDim.x);
   if (chunk < W) chunk = W;
   const int64_t a0 = blockIdx.x * chunk, a1 = min(a0 + chunk, total);
   if (a0 >= total) return;
-  const int64_t run = (a1 - a0 + W - 1) / W;
-  int64_t x = a0 + warp * run;
-  const int64_t xe = min(x + run, a1);
+  const int64_t run = quotient(a1 - a0 + W - 1, W);
+  const int64_t x = a0 + warp * run;
   if (lane < 2) piece[2 * warp + lane].r = -1;
 
-  if (x < xe) {
-    const char* const Kc = static_cast<const char*>(p.a.c.K);
-    const char* const Vc = static_cast<const char*>(p.a.c.V);
+  if (x < a1) {
+    const int32_t steps = static_cast<int32_t>(min(run, a1 - x));
     uint32_t bad = 0;
-    uint32_t row[S::RL], mask[S::RL], mask_n[S::RL], ex[S::RL], ex_n[S::RL];
-    uint32_t kf[TT][2][S::KV][4], vf[TT][4][S::VH][S::VR], qf[NT][D / 16][2];
+    uint32_t row[S::RL], ex[S::RL];
+    uint32_t qf[NT][MT][2];
     float sc[NT][2];               // logit scale of query heads 2c, 2c + 1
     float ref[NT][2], refw[NT][2]; // references of the sum and (8 bits) of the weights
     float sum[NT][2], o[NT][MT][4];
-
-    // rows of the step's tokens, a token per lane (or two)
-    auto look_up = [&](const Unit& v) {
-#pragma unroll
-      for (int i = 0; i < S::RL; ++i) {
-        const int32_t j = v.step * ST + (lane & (ST - 1)) + 32 * i;
-        row[i] = kNowhere;
-        if (E4) ex_n[i] = 0;
-        if (j < v.shown) {
-          const uint32_t pos = static_cast<uint32_t>(j >= p.a.sink ? j + v.shift : j);
-          const uint32_t at = pos / static_cast<uint32_t>(p.a.c.page_tokens), off = pos - at * p.a.c.page_tokens;
-          const int32_t id = __ldg(p.a.tables + v.r * p.a.table_stride + at);
-          if (id >= 0 && id < p.a.c.n_pages) {
-            row[i] = id * p.page16 + off * p.token16;
-            if (E4) {
-              const int64_t e = (static_cast<int64_t>(id) * p.a.c.n_kv_heads + heads_of<NT>(p, v.u).kv) * p.a.c.page_tokens + off;
-              ex_n[i] = __ldg(p.a.c.K_exp + e) | static_cast<uint32_t>(__ldg(p.a.c.V_exp + e)) << 8;
-            }
-          } else if (id != -1) {
-            bad = WK_DEV_BAD_SLOT;
-          }
-        }
-      }
-    };
-    auto load_k = [&](const Heads& h) {
-      const char* base = Kc + h.kv * p.head_bytes + c * 16;
-#pragma unroll
-      for (int t = 0; t < TT; ++t)
-#pragma unroll
-        for (int hh = 0; hh < 2; ++hh) {
-          const uint32_t at = S::RL == 1 ? __shfl_sync(0xffffffffu, row[0], t * 16 + hh * 8 + g)
-                                         : __shfl_sync(0xffffffffu, row[t * 16 / 32], (t * 16 + hh * 8 + g) & 31);
-          const char* src = base + static_cast<uint64_t>(at) * 16;
-#pragma unroll
-          for (int j = 0; j < S::KV; ++j) load16(kf[t][hh][j], src + 64 * j, at != kNowhere);
-        }
-    };
-    auto load_v = [&](const Heads& h) {
-      const char* base = Vc + h.kv * p.head_bytes + g * (4 * S::VR);
-#pragma unroll
-      for (int t = 0; t < TT; ++t)
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const int j = t * 16 + 2 * c + (k & 1) + (k >> 1) * 8;
-          const uint32_t at = S::RL == 1 ? __shfl_sync(0xffffffffu, row[0], j) : __shfl_sync(0xffffffffu, row[t * 16 / 32], j & 31);
-          const char* src = base + static_cast<uint64_t>(at) * 16;
-#pragma unroll
-          for (int hf = 0; hf < S::VH; ++hf) {
-            if constexpr (S::VR == 4) load16(vf[t][k][hf], src + 128 * hf, at != kNowhere);
-            else load8(vf[t][k][hf], src, at != kNowhere);
-          }
-        }
-    };
-    // Query row g of every tile, its dimensions in the order of the keys' loads.
-    auto load_q = [&](const Unit& v, const Heads& h) {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const bool on = nt * 8 + g < h.n;
-        const uint16_t* q = static_cast<const uint16_t*>(p.a.Q) + v.r * p.a.q_stride + static_cast<int64_t>(h.first + (on ? nt * 8 + g : 0)) * D;
-        constexpr int EPL = 16 / S::ES;   // elements of a key per 16-byte load
-#pragma unroll
-        for (int j = 0; j < S::KV; ++j)
-#pragma unroll
-          for (int e = 0; e < EPL / 8; ++e) {
-            uint4 w = make_uint4(0, 0, 0, 0);
-            if (on) w = *reinterpret_cast<const uint4*>(q + j * 4 * EPL + c * EPL + e * 8);
-            const int s = j * (EPL / 4) + 2 * e;
-            qf[nt][s][0] = w.x;
-            qf[nt][s][1] = w.y;
-            qf[nt][s + 1][0] = w.z;
-            qf[nt][s + 1][1] = w.w;
-          }
-      }
-    };
-    auto begin_unit = [&]() {
-#pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        if (E4) {
-          // row g by a power of two to below 2^15: exact in fp16 for all that matters beside the row's largest
-          float top = 0.f;
-#pragma unroll
-          for (int s = 0; s < D / 16; ++s)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) {
-              const float l = fabsf(lo_of(qf[nt][s][e], QBF)), h = fabsf(hi_of(qf[nt][s][e], QBF));
-              if (l <= 3.402823466e38f) top = fmaxf(top, l);
-              if (h <= 3.402823466e38f) top = fmaxf(top, h);
-            }
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-          top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-          const int power = max(static_cast<int>(__float_as_uint(top) >> 23), 28) - 127;   // floor(log2), at least -99
-          const float scale = __uint_as_float(static_cast<uint32_t>(14 - power + 127) << 23);
-          const float back = __uint_as_float(static_cast<uint32_t>(max(power - 14 + 127, 1)) << 23);
-#pragma unroll
-          for (int s = 0; s < D / 16; ++s)
-#pragma unroll
-            for (int e = 0; e < 2; ++e)
-              qf[nt][s][e] = pack2<false>(lo_of(qf[nt][s][e], QBF) * scale, hi_of(qf[nt][s][e], QBF) * scale);
-          sc[nt][0] = __shfl_sync(0xffffffffu, back, 8 * c) * (p.a.scale * 1.4426950408889634f);
-          sc[nt][1] = __shfl_sync(0xffffffffu, back, 8 * c + 4) * (p.a.scale * 1.4426950408889634f);
-        } else {
-          sc[nt][0] = sc[nt][1] = p.a.scale * 1.4426950408889634f;
-        }
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          ref[nt][e] = refw[nt][e] = -INFINITY;
-          sum[nt][e] = 0.f;
-        }
-#pragma unroll
-        for (int m = 0; m < MT; ++m)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) o[nt][m][e] = 0.f;
-      }
-    };
-
-    Unit cur = locate<ST, THREADS>(p, pre, per, x), nxt = cur;
+    Unit cur = locate<ST>(p, pre, per, x), nxt = cur;   // of the step at hand, of the next one to ask for
     Heads hc = heads_of<NT>(p, cur.u), hn = hc;
     int32_t began = cur.step;
     bool fresh = true;
-    look_up(cur);
-    load_q(cur, hc);
-    load_k(hc);
-    load_v(hc);
-#pragma unroll
-    for (int i = 0; i < S::RL; ++i) {
-      mask[i] = __ballot_sync(0xffffffffu, row[i] != kNowhere);
-      ex[i] = ex_n[i];
-    }
-    if (x + 1 < xe) {
-      advance<ST>(p, nxt);
-      hn = heads_of<NT>(p, nxt.u);
-      look_up(nxt);
-    }
+    const uint32_t ring_at = ptx::smem_u32(ring);
+    int slot = 0;
 
-    for (;; ++x) {
-      const bool more = x + 1 < xe;
-      const bool other = more && nxt.step == 0;   // the next step belongs to another unit
-      if (fresh) {
-        begin_unit();
-        fresh = false;
-      }
-      // ---- S^T = K Q^T
-      float s[TT][NT][4];
+#pragma unroll 1
+    for (int32_t i = -STAGES; i < steps; ++i) {
+      // ---- look up the rows of step i + STAGES, a token per lane (or two)
+      const bool ask = i + STAGES < steps;
+      if (ask) {
+        if (i > -STAGES) {
+          advance<ST>(p, nxt);
+          if (nxt.step == 0) hn = heads_of<NT>(p, nxt.u);
+        }
 #pragma unroll
-      for (int t = 0; t < TT; ++t)
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) s[t][nt][e] = 0.f;
-#pragma unroll
-          for (int j = 0; j < S::KV; ++j) {
-            if constexpr (E4) {
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                mma<false>(s[t][nt], codes_lo(kf[t][0][j][i]), codes_lo(kf[t][1][j][i]), codes_hi(kf[t][0][j][i]),
-                           codes_hi(kf[t][1][j][i]), qf[nt][4 * j + i][0], qf[nt][4 * j + i][1]);
-            } else {
-#pragma unroll
-              for (int i = 0; i < 2; ++i)
-                mma<BF>(s[t][nt], kf[t][0][j][2 * i], kf[t][1][j][2 * i], kf[t][0][j][2 * i + 1], kf[t][1][j][2 * i + 1],
-                        qf[nt][2 * j + i][0], qf[nt][2 * j + i][1]);
+        for (int k = 0; k < S::RL; ++k) {
+          const int32_t j = nxt.step * ST + (lane & (ST - 1)) + 32 * k;
+          row[k] = kNowhere;
+          ex[k] = 0;
+          if (j < nxt.shown) {
+            const uint32_t pos = static_cast<uint32_t>(j >= p.a.sink ? j + nxt.shift : j);
+            const uint32_t at = pos / static_cast<uint32_t>(p.a.c.page_tokens), off = pos - at * p.a.c.page_tokens;
+            const int32_t id = __ldg(p.a.tables + nxt.r * p.a.table_stride + at);
+            if (id >= 0 && id < p.a.c.n_pages) {
+              row[k] = id * p.page16 + off * p.token16;
+              if (E4) {
+                const int64_t e = (static_cast<int64_t>(id) * p.a.c.n_kv_heads + hn.kv) * p.a.c.page_tokens + off;
+                ex[k] = __ldg(p.a.c.K_exp + e) | static_cast<uint32_t>(__ldg(p.a.c.V_exp + e)) << 8;
+              }
+            } else if (id != -1) {
+              bad = WK_DEV_BAD_SLOT;
             }
           }
         }
-      if (more) {
-#pragma unroll
-        for (int i = 0; i < S::RL; ++i) mask_n[i] = __ballot_sync(0xffffffffu, row[i] != kNowhere);
-        if (other) load_q(nxt, hn);   // (Q of this unit is not needed any more)
-        load_k(hn);
       }
-      // ---- logits (log2), their largest, the references
-      float w[E4 ? TT : 1][NT][4];
-      float top[NT][2], topw[NT][2];
+
+      if (i >= 0) {
+        copies_wait<STAGES - 1>();
+        __syncwarp();
+        const uint32_t k_at = ring_at + slot * kStepBytes, v_at = k_at + kStepBytes / 2;
+        if (fresh) {   // a unit begins: Q has been asked for
+          fresh = false;
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) top[nt][0] = top[nt][1] = topw[nt][0] = topw[nt][1] = -INFINITY;
+          for (int nt = 0; nt < NT; ++nt) {
+            if (E4) {
+              // row g by a power of two to below 2^15: exact in fp16 for all that matters beside the row's largest
+              float top = 0.f;
 #pragma unroll
-      for (int t = 0; t < TT; ++t)
+              for (int s = 0; s < MT; ++s)
 #pragma unroll
-        for (int hh = 0; hh < 2; ++hh) {
-          const bool on = mask[S::RL == 1 ? 0 : t * 16 / 32] >> ((t * 16 + hh * 8 + g) & 31) & 1;
-          float kscale = 1.f, vpower = 0.f;
-          if (E4) {
-            const uint32_t e = __shfl_sync(0xffffffffu, ex[S::RL == 1 ? 0 : t * 16 / 32], (t * 16 + hh * 8 + g) & 31);
-            kscale = __uint_as_float((e & 255u) << 23);
-            vpower = static_cast<float>(static_cast<int>(e >> 8) - 127);
+                for (int e = 0; e < 2; ++e) {
+                  const float l = fabsf(lo_of(qf[nt][s][e], QBF)), h = fabsf(hi_of(qf[nt][s][e], QBF));
+                  if (l <= 3.402823466e38f) top = fmaxf(top, l);
+                  if (h <= 3.402823466e38f) top = fmaxf(top, h);
+                }
+              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+              top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+              const int power = max(static_cast<int>(__float_as_uint(top) >> 23), 28) - 127;   // floor(log2), at least -99
+              const float scale = __uint_as_float(static_cast<uint32_t>(14 - power + 127) << 23);
+              const float back = __uint_as_float(static_cast<uint32_t>(max(power - 14 + 127, 1)) << 23);
+#pragma unroll
+              for (int s = 0; s < MT; ++s)
+#pragma unroll
+                for (int e = 0; e < 2; ++e)
+                  qf[nt][s][e] = pack2<false>(lo_of(qf[nt][s][e], QBF) * scale, hi_of(qf[nt][s][e], QBF) * scale);
+              sc[nt][0] = __shfl_sync(0xffffffffu, back, 8 * c) * (p.a.scale * kLog2e);
+              sc[nt][1] = __shfl_sync(0xffffffffu, back, 8 * c + 4) * (p.a.scale * kLog2e);
+            } else {
+              sc[nt][0] = sc[nt][1] = p.a.scale * kLog2e;
+            }
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              ref[nt][e] = refw[nt][e] = -INFINITY;
+              sum[nt][e] = 0.f;
+            }
+#pragma unroll
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[nt][m][e] = 0.f;
           }
+        }
+        // ---- S^T = K Q^T.  A lane's place in the matrices that it points to: rows 0-7 and 8-15 of the left, then of the right 16 bytes
+        float s[ST / 16][NT][4];
+        {
+          const int r8 = lane & 7, sw = ROW == 64 ? r8 >> 1 : r8;
+          const uint32_t at = k_at + ((lane >> 3 & 1) * 8 + r8) * ROW + (((lane >> 4) ^ sw) << 4);
+#pragma unroll
+          for (int t = 0; t < ST / 16; ++t) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) s[t][nt][e] = 0.f;
+#pragma unroll
+            for (int j = 0; j < ROW / 32; ++j) {
+              uint32_t f[4];
+              load_matrices<false>(f, (at + t * 16 * ROW) ^ (j << 5));
+              if constexpr (E4) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                  const uint32_t f0 = codes_lo(f[2 * h]), f1 = codes_lo(f[2 * h + 1]), f2 = codes_hi(f[2 * h]), f3 = codes_hi(f[2 * h + 1]);
+#pragma unroll
+                  for (int nt = 0; nt < NT; ++nt) mma<false>(s[t][nt], f0, f1, f2, f3, qf[nt][2 * j + h][0], qf[nt][2 * j + h][1]);
+                }
+              } else {
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma<BF>(s[t][nt], f[0], f[1], f[2], f[3], qf[nt][j][0], qf[nt][j][1]);
+              }
+            }
+          }
+        }
+        // ---- logits (log2), their largest, the references
+        float w[E4 ? ST / 16 : 1][NT][4];
+        float top[NT][2], topw[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) top[nt][0] = top[nt][1] = topw[nt][0] = topw[nt][1] = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < ST / 16; ++t) {
+          const uint32_t mask = masks[warp][slot][t / 2] >> (t % 2 * 16 + g);
+#pragma unroll
+          for (int hh = 0; hh < 2; ++hh) {
+            const bool on = mask >> (8 * hh) & 1;
+            float kscale = 1.f, vpower = 0.f;
+            if (E4) {
+              const uint32_t e = exps[slot * ST + t * 16 + hh * 8 + g];
+              kscale = __uint_as_float((e & 255u) << 23);
+              vpower = static_cast<float>(static_cast<int>(e >> 8) - 127);
+            }
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) {
+                float& v = s[t][nt][2 * hh + e];
+                v = on ? v * (E4 ? sc[nt][e] * kscale : sc[nt][e]) : -INFINITY;
+                top[nt][e] = fmaxf(top[nt][e], v);
+                if constexpr (E4) {
+                  w[t][nt][2 * hh + e] = v + vpower;
+                  topw[nt][e] = fmaxf(topw[nt][e], v + vpower);
+                }
+              }
+          }
+        }
+        bool moved = false;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) moved |= top[nt][e] > ref[nt][e] + kLazy || (E4 && topw[nt][e] > refw[nt][e] + kLazy);
+        if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              float& v = s[t][nt][2 * hh + e];
-              v = on ? v * (E4 ? sc[nt][e] * kscale : sc[nt][e]) : -INFINITY;
-              top[nt][e] = fmaxf(top[nt][e], v);
-              if constexpr (E4) {
-                w[t][nt][2 * hh + e] = v + vpower;
-                topw[nt][e] = fmaxf(topw[nt][e], v + vpower);
+              float m = fmaxf(top[nt][e], ref[nt][e]), mw = fmaxf(topw[nt][e], refw[nt][e]);
+#pragma unroll
+              for (int d = 4; d < 32; d <<= 1) {
+                m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+                if (E4) mw = fmaxf(mw, __shfl_xor_sync(0xffffffffu, mw, d));
+              }
+              const float f = m == -INFINITY ? 1.f : ex2_approx(ref[nt][e] - m);
+              sum[nt][e] *= f;
+              ref[nt][e] = m;
+              float fw = f;
+              if (E4) {
+                fw = mw == -INFINITY ? 1.f : ex2_approx(refw[nt][e] - mw);
+                refw[nt][e] = mw;
+              }
+#pragma unroll
+              for (int mt = 0; mt < MT; ++mt) {
+                o[nt][mt][e] *= fw;
+                o[nt][mt][2 + e] *= fw;
               }
             }
         }
-      bool moved = false;
+        // ---- weights, and O^T += V^T P^T
+        const int r8 = lane & 7, sw = ROW == 64 ? r8 >> 1 : r8;
+        const uint32_t at = v_at + ((lane >> 4) * 8 + r8) * ROW + (((lane >> 3 & 1) ^ sw) << 4);
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+        for (int t = 0; t < ST / 16; ++t) {
+          uint32_t pf[NT][2];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) moved |= top[nt][e] > ref[nt][e] + kLazy || (E4 && topw[nt][e] > refw[nt][e] + kLazy);
-      if (__any_sync(0xffffffffu, moved)) {
+          for (int nt = 0; nt < NT; ++nt) {
+            float q[4];
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            float m = fmaxf(top[nt][e], ref[nt][e]), mw = fmaxf(topw[nt][e], refw[nt][e]);
-#pragma unroll
-            for (int d = 4; d < 32; d <<= 1) {
-              m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-              if (E4) mw = fmaxf(mw, __shfl_xor_sync(0xffffffffu, mw, d));
+            for (int e = 0; e < 4; ++e) {
+              q[e] = ex2_approx(s[t][nt][e] - (ref[nt][e & 1] == -INFINITY ? 0.f : ref[nt][e & 1]));
+              sum[nt][e & 1] += q[e];
+              if constexpr (E4) q[e] = ex2_approx(w[t][nt][e] - (refw[nt][e & 1] == -INFINITY ? 0.f : refw[nt][e & 1]));
             }
-            const float f = m == -INFINITY ? 1.f : exp2_of(ref[nt][e] - m);
-            sum[nt][e] *= f;
-            ref[nt][e] = m;
-            float fw = f;
-            if (E4) {
-              fw = mw == -INFINITY ? 1.f : exp2_of(refw[nt][e] - mw);
-              refw[nt][e] = mw;
-            }
-#pragma unroll
-            for (int mt = 0; mt < MT; ++mt) {
-              o[nt][mt][e] *= fw;
-              o[nt][mt][2 + e] *= fw;
-            }
+            pf[nt][0] = transpose8x8(pack2<BF>(q[0], q[1]));
+            pf[nt][1] = transpose8x8(pack2<BF>(q[2], q[3]));
           }
-      }
-      // ---- weights, and O^T += V^T P^T
 #pragma unroll
-      for (int t = 0; t < TT; ++t) {
-        uint32_t pf[NT][2];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          float q[4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const float r = ref[nt][e & 1] == -INFINITY ? 0.f : ref[nt][e & 1];
-            q[e] = exp2_of(s[t][nt][e] - r);
-            sum[nt][e & 1] += q[e];
-            if constexpr (E4) q[e] = exp2_of(w[t][nt][e] - (refw[nt][e & 1] == -INFINITY ? 0.f : refw[nt][e & 1]));
-          }
-          pf[nt][0] = transpose8x8(pack2<BF>(q[0], q[1]));
-          pf[nt][1] = transpose8x8(pack2<BF>(q[2], q[3]));
-        }
-#pragma unroll
-        for (int hf = 0; hf < S::VH; ++hf)
-#pragma unroll
-          for (int i = 0; i < S::VR; ++i) {
-            if constexpr (E4) {
+          for (int j = 0; j < ROW / 32; ++j) {
+            uint32_t f[4];
+            load_matrices<true>(f, (at + t * 16 * ROW) ^ (j << 5));
+            if constexpr (E4) {   // pairs of neighbouring dimensions of two tokens: to pairs of tokens
 #pragma unroll
               for (int h = 0; h < 2; ++h) {
-                const uint32_t sel = h ? 0x7362u : 0x5140u;
-                const uint32_t x01 = __byte_perm(vf[t][0][hf][i], vf[t][1][hf][i], sel);
-                const uint32_t x23 = __byte_perm(vf[t][2][hf][i], vf[t][3][hf][i], sel);
-                const uint32_t f0 = codes_lo(x01), f1 = codes_hi(x01), f2 = codes_lo(x23), f3 = codes_hi(x23);
+                const uint32_t x0 = __byte_perm(f[h], 0, 0x3120), x1 = __byte_perm(f[2 + h], 0, 0x3120);
+                const uint32_t f0 = codes_lo(x0), f1 = codes_hi(x0), f2 = codes_lo(x1), f3 = codes_hi(x1);
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma<false>(o[nt][2 * i + h], f0, f1, f2, f3, pf[nt][0], pf[nt][1]);
+                for (int nt = 0; nt < NT; ++nt) mma<false>(o[nt][2 * j + h], f0, f1, f2, f3, pf[nt][0], pf[nt][1]);
               }
             } else {
-              const uint32_t f0 = __byte_perm(vf[t][0][hf][i], vf[t][1][hf][i], 0x5410);
-              const uint32_t f1 = __byte_perm(vf[t][0][hf][i], vf[t][1][hf][i], 0x7632);
-              const uint32_t f2 = __byte_perm(vf[t][2][hf][i], vf[t][3][hf][i], 0x5410);
-              const uint32_t f3 = __byte_perm(vf[t][2][hf][i], vf[t][3][hf][i], 0x7632);
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt) mma<BF>(o[nt][4 * hf + i], f0, f1, f2, f3, pf[nt][0], pf[nt][1]);
+              for (int nt = 0; nt < NT; ++nt) mma<BF>(o[nt][j], f[0], f[1], f[2], f[3], pf[nt][0], pf[nt][1]);
             }
           }
+        }
       }
-      if (more) load_v(hn);
 
-      // ---- the unit ends here, or this warp's part of it
-      if (!more || other) {
-        const bool whole = began == 0 && cur.step == cur.cost - 1;
-        const int slot = 2 * warp + (began == 0);   // reaches in: the warp's first unit; out: its last
+      // ---- ask for the rows just looked up, in the place of the step just used
+      __syncwarp();
+      if (ask) {
+        const uint32_t to = ring_at + slot * kStepBytes;
+        const char* const kb = static_cast<const char*>(p.a.c.K) + hn.kv * p.head_bytes + lane % S::LPR * 16;
+        const char* const vb = static_cast<const char*>(p.a.c.V) + hn.kv * p.head_bytes + lane % S::LPR * 16;
+        const uint32_t chunk = lane % S::LPR;
+#pragma unroll 2
+        for (int k = 0; k < 8; ++k) {
+          const int token = k * S::RPI + lane / S::LPR;
+          const uint32_t at = __shfl_sync(0xffffffffu, S::RL == 1 || k < 4 ? row[0] : row[S::RL - 1], token & 31);
+          const uint32_t skip = at == kNowhere;
+          const uint64_t src = static_cast<uint64_t>(skip ? 0 : at) * 16;
+          const uint32_t dst = to + token * ROW + ((chunk ^ (ROW == 64 ? token >> 1 & 3 : token & 7)) << 4);
+          copy16(dst, kb + src, skip);
+          copy16(dst + kStepBytes / 2, vb + src, skip);
+        }
+#pragma unroll
+        for (int k = 0; k < S::RL; ++k) {
+          const uint32_t mask = __ballot_sync(0xffffffffu, row[k] != kNowhere);
+          if (lane == 0) masks[warp][slot][k] = mask;
+          if (E4) exps[slot * ST + (lane & (ST - 1)) + 32 * k] = static_cast<uint16_t>(ex[k]);
+        }
+      }
+      copies_commit();
+      if (++slot == STAGES) slot = 0;
+
+      // ---- does the unit end here, or this warp's part of it?
+      const bool ends = i >= 0 && (i + 1 == steps || cur.step + 1 == cur.cost);
+      const Unit was = cur;
+      const Heads hw = hc;
+      if (i >= 0 && i + 1 < steps) {
+        advance<ST>(p, cur);
+        if (ends) hc = heads_of<NT>(p, cur.u);
+      }
+      float f[NT][2];
+      if (ends) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -542,166 +561,229 @@ paged_attention(const __grid_constant__ Params p) {
             float l = sum[nt][e];
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
-            const float lse = l == 0.f ? -INFINITY : ref[nt][e] + __log2f(l);
-            const float f = l == 0.f ? 0.f : E4 ? exp2f(refw[nt][e] - ref[nt][e]) / l : 1.f / l;
-            const int q = nt * 8 + 2 * c + e;
-            if (q < hc.n) {
-              // runs of dimensions that a lane holds: 8 from 64 hf + 8 g on, or (8 bits) D / 8 from g D / 8 on
-              constexpr int RUN = E4 ? D / 8 : 8;
+            sum[nt][e] = l == 0.f ? -INFINITY : ref[nt][e] + __log2f(l);   // log-sum-exp (log2)
+            f[nt][e] = l == 0.f ? 0.f : __fdividef(E4 ? ex2_approx(refw[nt][e] - ref[nt][e]) : 1.f, l);
+          }
+      }
+      if (ends ? i + 1 < steps : i == -1) {   // Q of the unit that comes next: row g of every tile
+        fresh = true;
 #pragma unroll
-              for (int k = 0; k < D / 8 / 8; ++k) {
-                const int d0 = E4 ? g * RUN + 8 * k : 64 * k + 8 * g;
-                float v[8];
+        for (int nt = 0; nt < NT; ++nt) {
+          const bool on = nt * 8 + g < hc.n;
+          const uint16_t* q = static_cast<const uint16_t*>(p.a.Q) + cur.r * p.a.q_stride + static_cast<int64_t>(hc.first + (on ? nt * 8 + g : 0)) * D;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                  v[2 * i] = o[nt][4 * k + i][e] * f;
-                  v[2 * i + 1] = o[nt][4 * k + i][2 + e] * f;
-                }
-                if (whole) {
-                  const int64_t at = (static_cast<int64_t>(cur.r) * p.a.n_heads + hc.first + q) * D + d0;
-                  *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.a.O) + at) =
-                      make_uint4(pack2<QBF>(v[0], v[1]), pack2<QBF>(v[2], v[3]), pack2<QBF>(v[4], v[5]), pack2<QBF>(v[6], v[7]));
-                } else {
-                  float4* to = reinterpret_cast<float4*>(po + (slot * 8 * NT + q) * PADDED + d0);
-                  to[0] = make_float4(v[0], v[1], v[2], v[3]);
-                  to[1] = make_float4(v[4], v[5], v[6], v[7]);
-                }
-              }
-              if (g == 0) {
-                if (!whole) plse[slot][q] = lse;
-                else if (p.a.lse) p.a.lse[static_cast<int64_t>(cur.r) * p.a.n_heads + hc.first + q] = lse * kLn2;
-              }
+          for (int m = 0; m < MT; ++m) {
+            if (E4) {
+              const uint2 v = on ? *reinterpret_cast<const uint2*>(q + m * 16 + 4 * c) : make_uint2(0, 0);
+              qf[nt][m][0] = v.x;
+              qf[nt][m][1] = v.y;
+            } else {
+#pragma unroll
+              for (int e = 0; e < 2; ++e) qf[nt][m][e] = on ? *reinterpret_cast<const uint32_t*>(q + m * 16 + 8 * e + 2 * c) : 0u;
             }
           }
-        if (!whole && lane == 0) piece[slot] = Piece{cur.r, cur.u, cur.cost, x - cur.step};
+        }
+      }
+      if (ends) {
+        const bool whole = began == 0 && was.step + 1 == was.cost;
+        const int which = 2 * warp + (began == 0);   // reaches in: the warp's first unit; out: its last
         began = 0;
-        fresh = true;
-      }
-      if (!more) break;
-      cur = nxt;
-      hc = hn;
+        if (whole) {
+          // transposed in registers: lane (g, c) then has head g's dimensions 2c, 2c + 1 of every 8 (8 bits: 4c .. 4c + 3 of 16)
 #pragma unroll
-      for (int i = 0; i < S::RL; ++i) {
-        mask[i] = mask_n[i];
-        ex[i] = ex_n[i];
-      }
-      if (x + 2 < xe) {
-        advance<ST>(p, nxt);
-        if (nxt.step == 0) hn = heads_of<NT>(p, nxt.u);
-        look_up(nxt);
+          for (int nt = 0; nt < NT; ++nt) {
+            const int64_t head = static_cast<int64_t>(was.r) * p.a.n_heads + hw.first + nt * 8;
+            uint16_t* const to = static_cast<uint16_t*>(p.a.O) + (head + g) * D;
+#pragma unroll
+            for (int m = 0; m < MT; ++m) {
+              const uint32_t y0 = transpose8x8(pack2<QBF>(o[nt][m][0] * f[nt][0], o[nt][m][1] * f[nt][1]));
+              const uint32_t y1 = transpose8x8(pack2<QBF>(o[nt][m][2] * f[nt][0], o[nt][m][3] * f[nt][1]));
+              if (nt * 8 + g < hw.n) {
+                if (E4) {
+                  *reinterpret_cast<uint2*>(to + m * 16 + 4 * c) = make_uint2(__byte_perm(y0, y1, 0x5410), __byte_perm(y0, y1, 0x7632));
+                } else {
+                  *reinterpret_cast<uint32_t*>(to + m * 16 + 2 * c) = y0;
+                  *reinterpret_cast<uint32_t*>(to + m * 16 + 8 + 2 * c) = y1;
+                }
+              }
+            }
+            if (g == 0 && p.a.lse) {
+#pragma unroll
+              for (int e = 0; e < 2; ++e)
+                if (nt * 8 + 2 * c + e < hw.n) p.a.lse[head + 2 * c + e] = sum[nt][e] * kLn2;
+            }
+          }
+        } else {
+          float* const rows = piece_rows(which);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+              const int q = nt * 8 + 2 * c + e;
+              if (q >= hw.n) continue;
+#pragma unroll
+              for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                  rows[q * PADDED + m * 16 + (E4 ? 2 * g + h : 8 * h + g)] = o[nt][m][2 * h + e] * f[nt][e];
+              if (g == 0) plse[which][q] = sum[nt][e];
+            }
+          if (lane == 0) piece[which] = Piece{was.r, was.u, was.cost, x + i - was.step};
+        }
       }
     }
     if (bad && p.a.status) atomicOr(p.a.status, bad);
   }
-  if (tid < 2) split[tid].r = -1;
   __syncthreads();
 
-  // ---- pieces of one unit, next to each other: joined into O, or into this CTA's piece
+  // ---- pieces of one unit lie next to each other: joined into O, or into this CTA's piece.  A warp takes a row at a time.
   float* const partial = reinterpret_cast<float*>(p.a.scratch + p.counter_bytes);
-  for (int i0 = 0; i0 < 2 * W;) {
-    if (piece[i0].r < 0) {
-      ++i0;
-      continue;
+  if (warp == 0) {
+    static_assert(2 * kMaxWarps <= 32, "a lane per piece");
+    const bool there = lane < 2 * W && piece[lane].r >= 0;
+    const uint32_t below = __ballot_sync(0xffffffffu, there) & ((1u << lane) - 1);
+    const int prev = below ? 31 - __clz(below) : lane;
+    const bool start = there && (prev == lane || piece[prev].r != piece[lane].r || piece[prev].u != piece[lane].u);
+    const uint32_t starts = __ballot_sync(0xffffffffu, start);
+    if (lane < 2) split[lane].r = -1;
+    __syncwarp();
+    if (start) {
+      const Piece u = piece[lane];
+      group_at[__popc(starts & ((1u << lane) - 1))] = lane;
+      if (u.start < a0) split[0] = u;
+      else if (u.start + u.cost > a1) split[1] = u;
     }
-    const Piece u = piece[i0];
-    int i1 = i0 + 1;
-    while (i1 < 2 * W && (piece[i1].r < 0 || (piece[i1].r == u.r && piece[i1].u == u.u))) ++i1;
-    const Heads h = heads_of<NT>(p, u.u);
-    const bool whole = u.start >= a0 && u.start + u.cost <= a1;
-    const int side = u.start < a0 ? 0 : 1;
-    float* const mine_at = partial + static_cast<int64_t>(2 * blockIdx.x + side) * kPieceFloats;
-    for (int it = tid; it < h.n * (D / 4); it += THREADS) {
-      const int q = it / (D / 4), d4 = it % (D / 4);
-      float m = -INFINITY;
-      for (int i = i0; i < i1; ++i)
-        if (piece[i].r >= 0) m = fmaxf(m, plse[i][q]);
-      if (m == -INFINITY) m = 0.f;
-      float l = 0.f;
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int i = i0; i < i1; ++i)
-        if (piece[i].r >= 0) {
-          const float e = exp2_of(plse[i][q] - m);
-          const float4 b = *reinterpret_cast<const float4*>(po + (i * 8 * NT + q) * PADDED + 4 * d4);
-          l += e;
-          v.x += e * b.x; v.y += e * b.y; v.z += e * b.z; v.w += e * b.w;
-        }
-      const float f = l == 0.f ? 0.f : 1.f / l, lse = l == 0.f ? -INFINITY : m + __log2f(l);
-      v.x *= f; v.y *= f; v.z *= f; v.w *= f;
-      if (whole) {
-        const int64_t at = static_cast<int64_t>(u.r) * p.a.n_heads + h.first + q;
-        store4<QBF>(p.a.O, at * D + 4 * d4, v);
-        if (d4 == 0 && p.a.lse) p.a.lse[at] = lse * kLn2;
-      } else {
-        *reinterpret_cast<float4*>(mine_at + 8 * NT + q * D + 4 * d4) = v;
-        if (d4 == 0) mine_at[q] = lse;
-      }
+    if (lane == 0) {
+      n_groups = __popc(starts);
+      group_at[__popc(starts)] = 2 * W;
     }
-    if (!whole && tid == 0) split[side] = u;
-    i0 = i1;
   }
+  __syncthreads();
+  using Vec = typename Lane<D>::Vec;       // a lane's part of a row
+  const int rows = min(8 * NT, p.group);   // query heads of a full unit
+#pragma unroll 1
+  for (int it = warp; it < n_groups * rows; it += W) {
+    const int k = it / rows, q = it - k * rows;
+    const int i0 = group_at[k], i1 = group_at[k + 1];
+    const Piece u = piece[i0];
+    const Heads h = heads_of<NT>(p, u.u);
+    if (q >= h.n) continue;
+    const bool there = i0 + lane < i1 && piece[i0 + lane].r >= 0;   // (fewer than 32 pieces)
+    float l = there ? plse[i0 + lane][q] : -INFINITY;
+    const float e = join_weight(l);
+    Vec v = {};
+#pragma unroll 1
+    for (uint32_t m = __ballot_sync(0xffffffffu, there); m; m &= m - 1) {
+      const int i = __ffs(m) - 1;
+      Lane<D>::add(v, __shfl_sync(0xffffffffu, e, i), reinterpret_cast<const Vec*>(piece_rows(i0 + i) + q * PADDED)[lane]);
+    }
+    if (u.start >= a0 && u.start + u.cost <= a1) {
+      const int64_t at = static_cast<int64_t>(u.r) * p.a.n_heads + h.first + q;
+      Lane<D>::template store<QBF>(p.a.O, at * D, lane, v);
+      if (lane == 0 && p.a.lse) p.a.lse[at] = l * kLn2;
+    } else {
+      float* const to = partial + static_cast<int64_t>(2 * blockIdx.x + (u.start < a0 ? 0 : 1)) * kPieceFloats;
+      reinterpret_cast<Vec*>(to + 8 * NT + q * D)[lane] = v;
+      if (lane == 0) to[q] = l;
+    }
+  }
+  if (split[0].r < 0 && split[1].r < 0) return;
 
   // ---- units that other CTAs share: the last of them to arrive joins the pieces
-  __threadfence();
   __syncthreads();
-  uint32_t* const arrived = reinterpret_cast<uint32_t*>(p.a.scratch);
   if (tid < 2) {
-    last[tid] = 0;
+    count[tid] = 0;
     if (split[tid].r >= 0) {
-      const int64_t first = split[tid].start / chunk, end = (split[tid].start + split[tid].cost - 1) / chunk;
-      const uint32_t n = static_cast<uint32_t>(end - first);
-      last[tid] = atomicInc(arrived + first, n) == n;
+      first[tid] = static_cast<int>(quotient(split[tid].start, chunk));
+      const uint32_t n = static_cast<uint32_t>(quotient(split[tid].start + split[tid].cost - 1, chunk)) - first[tid];
+      __threadfence();   // the barrier has ordered the CTA's pieces before this
+      if (atomicInc(reinterpret_cast<uint32_t*>(p.a.scratch) + first[tid], n) == n) count[tid] = n + 1;
       __threadfence();
     }
   }
   __syncthreads();
+  Vec* const part = reinterpret_cast<Vec*>(dyn);   // [W][32]
+  float* const sums = reinterpret_cast<float*>(dyn + W * 32 * sizeof(Vec));   // [W][2]
+#pragma unroll 1
   for (int side = 0; side < 2; ++side) {
-    if (!last[side]) continue;
+    const int n = count[side];
+    if (n == 0) continue;
     const Piece u = split[side];
     const Heads h = heads_of<NT>(p, u.u);
-    const int first = static_cast<int>(u.start / chunk), n = static_cast<int>((u.start + u.cost - 1) / chunk) - first + 1;
-    auto piece_at = [&](int i) -> const float* {   // the unit's first CTA has it as its last unit, the others as their first
-      return partial + static_cast<int64_t>(2 * (first + i) + (u.start < (first + i) * chunk ? 0 : 1)) * kPieceFloats;
-    };
-    for (int it = tid; it < h.n * (D / 4); it += THREADS) {
-      const int q = it / (D / 4), d4 = it % (D / 4);
-      float m = -INFINITY;
-      for (int i = 0; i < n; ++i) m = fmaxf(m, __ldcg(piece_at(i) + q));
-      if (m == -INFINITY) m = 0.f;
-      float l = 0.f;
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-      for (int i = 0; i < n; ++i) {
-        const float* from = piece_at(i);
-        const float e = exp2_of(__ldcg(from + q) - m);
-        const float4 b = __ldcg(reinterpret_cast<const float4*>(from + 8 * NT + q * D) + d4);
-        l += e;
-        v.x += e * b.x; v.y += e * b.y; v.z += e * b.z; v.w += e * b.w;
+    // A row belongs to one warp, or to several that take the pieces in turn.  The unit's first CTA has it as its last unit, the others
+    // as their first.
+    const int sets = max(W / h.n, 1);
+#pragma unroll 1
+    for (int q0 = 0; q0 < h.n; q0 += W / sets) {
+      const int q = q0 + warp / sets, set = warp % sets;
+      const bool on = q < h.n && warp < W / sets * sets;
+      Vec v = {};
+      float top = -INFINITY, l = 0.f;   // of this warp's pieces
+      if (on) {
+        const float* at = partial + (2 * first[side] + 1) * static_cast<int64_t>(kPieceFloats);
+#pragma unroll 1
+        for (int i0 = set; i0 < n; i0 += 32 * sets) {   // 32 of the pieces at a time
+          const int mine = i0 + lane * sets;
+          const float lse = mine < n ? __ldcg(at + (mine ? 2 * mine - 1 : 0) * static_cast<int64_t>(kPieceFloats) + q) : -INFINITY;
+          float m = lse;
+#pragma unroll
+          for (int d = 1; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
+          m = fmaxf(m, top);
+          const float keep = m == -INFINITY ? 1.f : ex2_approx(top - m), e = ex2_approx(lse - (m == -INFINITY ? 0.f : m));
+          top = m;
+          float s = e;
+#pragma unroll
+          for (int d = 1; d < 32; d <<= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+          l = l * keep + s;
+          Lane<D>::scale(v, keep);
+          const int in = min((n - i0 + sets - 1) / sets, 32);
+#pragma unroll 4
+          for (int k = 0; k < in; ++k) {
+            const int i = i0 + k * sets;
+            Lane<D>::add(v, __shfl_sync(0xffffffffu, e, k),
+                         __ldcg(reinterpret_cast<const Vec*>(at + (i ? 2 * i - 1 : 0) * static_cast<int64_t>(kPieceFloats) + 8 * NT + q * D) + lane));
+          }
+        }
+        part[warp * 32 + lane] = v;
+        if (lane == 0) {
+          sums[2 * warp] = l == 0.f ? -INFINITY : top + __log2f(l);
+          sums[2 * warp + 1] = l == 0.f ? 0.f : __fdividef(1.f, l);
+        }
       }
-      const float f = l == 0.f ? 0.f : 1.f / l, lse = l == 0.f ? -INFINITY : m + __log2f(l);
-      v.x *= f; v.y *= f; v.z *= f; v.w *= f;
-      const int64_t at = static_cast<int64_t>(u.r) * p.a.n_heads + h.first + q;
-      store4<QBF>(p.a.O, at * D + 4 * d4, v);
-      if (d4 == 0 && p.a.lse) p.a.lse[at] = lse * kLn2;
+      __syncthreads();
+      if (on && set == 0) {
+        float lse = lane < sets ? sums[2 * (warp + lane)] : -INFINITY;
+        const float e = join_weight(lse) * (lane < sets ? sums[2 * (warp + lane) + 1] : 0.f);
+        Vec w = {};
+#pragma unroll 1
+        for (int k = 0; k < sets; ++k) Lane<D>::add(w, __shfl_sync(0xffffffffu, e, k), part[(warp + k) * 32 + lane]);
+        const int64_t to = static_cast<int64_t>(u.r) * p.a.n_heads + h.first + q;
+        Lane<D>::template store<QBF>(p.a.O, to * D, lane, w);
+        if (lane == 0 && p.a.lse) p.a.lse[to] = lse * kLn2;
+      }
+      __syncthreads();
     }
   }
 }
 
-template <int MODE, int D, int NT, bool QBF>
-wk_status launch(wk_ctx* ctx, const Params& p, cudaStream_t s) {
+template <int MODE, int D, int NT, bool QBF, int STAGES>
+wk_status launch(wk_ctx* ctx, const Params& p, int warps, cudaStream_t s) {
   using S = Shape<MODE, D, NT>;
+  const int smem = warps * (STAGES * kStepBytes + S::PIECE + STAGES * S::META);
   const int i = ((MODE * 2 + (D == 128)) * 2 + NT - 1) * 2 + QBF;
-  if (!(ctx->paged_attr_set >> i & 1)) {
-    WK_CUDA_TRY(ctx, cudaFuncSetAttribute(paged_attention<MODE, D, NT, QBF>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::SMEM));
-    ctx->paged_attr_set |= 1u << i;
+  if (ctx->paged_smem[i] < smem) {
+    WK_CUDA_TRY(ctx, cudaFuncSetAttribute(paged_attention<MODE, D, NT, QBF, STAGES>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    ctx->paged_smem[i] = smem;
   }
-  paged_attention<MODE, D, NT, QBF><<<ctx->sm_count, 32 * S::W, S::SMEM, s>>>(p);
+  paged_attention<MODE, D, NT, QBF, STAGES><<<ctx->sm_count, 32 * warps, smem, s>>>(p);
   return after_launch(ctx);
 }
 
 template <int MODE, bool QBF>
 wk_status choose(wk_ctx* ctx, const Params& p, int nt, cudaStream_t s) {
-  if (p.a.c.head_dim == 128) return nt == 1 ? launch<MODE, 128, 1, QBF>(ctx, p, s) : launch<MODE, 128, 2, QBF>(ctx, p, s);
-  return nt == 1 ? launch<MODE, 64, 1, QBF>(ctx, p, s) : launch<MODE, 64, 2, QBF>(ctx, p, s);
+  const int warps = nt == 1 ? 10 : 8;
+  if (p.a.c.head_dim == 128) return nt == 1 ? launch<MODE, 128, 1, QBF, 2>(ctx, p, warps, s) : launch<MODE, 128, 2, QBF, 2>(ctx, p, warps, s);
+  return nt == 1 ? launch<MODE, 64, 1, QBF, 2>(ctx, p, warps, s) : launch<MODE, 64, 2, QBF, 2>(ctx, p, warps, s);
 }
 
 }  // namespace
