@@ -81,7 +81,7 @@ struct wk_ctx {
   size_t tmap_cache_next = 0;
   // per-context (hence per-device) one-time kernel attributes: opt-ins to large dynamic shared memory
   bool attn_attr_set = false;
-  int paged_smem[32] = {};       // dynamic shared memory that each variant of the paged attention has been let have
+  uint32_t paged_attr_set = 0;   // a bit per variant of the paged attention
   uint32_t compress_epoch = 0;   // call counter of the one-launch compression: its `ready` words compare against it
   // diagnostics
   int32_t last_cuda_error = 0;

@@ -35,7 +35,6 @@ constexpr uint32_t kNowhere = 0xffffffffu;   // row offset of a token that is no
 constexpr float kLazy = 8.f;                 // how far (log2) a logit may exceed the reference
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 constexpr int kStepBytes = 8192;             // of K and V in a step
-constexpr int kMaxWarps = 12;
 
 struct Params {
   PagedArgs a;
@@ -48,6 +47,10 @@ struct Params {
 
 template <int MODE, int D, int NT>
 struct Shape {
+  // Warps: as few as keep the memory busy, for fewer copies in flight are served more evenly (8: 203 us for 1.35 GB, 10: 213), and
+  // as many as the ring leaves room for where arithmetic counts too (8 bits: 6 warps 275 us for 0.92 GB, 8: 224, 10: 198).
+  static constexpr int W = MODE == WK_E4M3 && NT == 1 ? 10 : 8;
+  static constexpr int STAGES = 2;
   static constexpr int ES = MODE == WK_E4M3 ? 1 : 2;     // bytes per element of the cache
   static constexpr int ROW = D * ES;                     // bytes of a row
   static constexpr int ST = kStepBytes / 2 / ROW;        // tokens of a step: 16, 32 or 64
@@ -118,6 +121,7 @@ __device__ __forceinline__ float hi_of(uint32_t w, bool bf16) {
 using ptx::ex2_approx;
 
 // ---------------------------------------------------------------- units
+// The line: for every unit of a request (kv heads first) the steps of all requests, one after the other.
 struct Unit {
   int32_t r, u;         // request, unit of the request
   int32_t step, cost;   // place in the unit, steps of the unit (at least one, also where nothing is visible)
@@ -135,34 +139,32 @@ __device__ __forceinline__ int32_t measure(const Params& p, int r, int32_t* show
   return *shown > ST ? static_cast<int32_t>((static_cast<uint32_t>(*shown) + ST - 1) / ST) : 1;
 }
 
-// a / b of numbers that hardly ever need 64 bits.  (One copy of the long way: a CTA runs most of this kernel's code once, and
-// fetching instructions is then a good part of what that costs.)
+// a / b of numbers that hardly ever need 64 bits
 __device__ __noinline__ int64_t quotient64(int64_t a, int64_t b) { return a / b; }
 __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
   return (a | b) >> 32 ? quotient64(a, b) : static_cast<int64_t>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b));
 }
 
-// The unit that place x of the line lies in.  pre[t]: steps of one unit of each request before thread t's `per` requests.
-template <int ST>
-__device__ __forceinline__ Unit locate(const Params& p, const int64_t* pre, int per, int64_t x) {
-  const int64_t z = quotient(x, p.units);
-  int lo = -1;   // (the whole warp is here)
-#pragma unroll 4
-  for (int k = 0; k < blockDim.x; k += 32) lo += __popc(__ballot_sync(0xffffffffu, pre[k + (threadIdx.x & 31)] <= z));
+// The unit that place x of the line lies in.  pre[t]: steps of the requests before thread t's `per` requests, of all: `all`.
+template <int ST, int THREADS>
+__device__ __forceinline__ Unit locate(const Params& p, const uint32_t* pre, int per, uint32_t all, int64_t x) {
   Unit v;
-  int64_t before = pre[lo];
+  v.u = static_cast<int32_t>(quotient(x, all));
+  const uint32_t z = static_cast<uint32_t>(x - static_cast<int64_t>(v.u) * all);
+  int lo = -1;   // (the whole warp is here)
+#pragma unroll
+  for (int k = 0; k < THREADS; k += 32) lo += __popc(__ballot_sync(0xffffffffu, pre[k + (threadIdx.x & 31)] <= z));
+  uint32_t before = pre[lo];
   v.r = lo * per;
   v.shown = v.shift = 0;
   v.cost = measure<ST>(p, v.r, &v.shown, &v.shift);
 #pragma unroll 1
-  while (before + v.cost <= z && v.r < p.a.n_req - 1) {   // (z lies before the sum of all: the second bound is for lengths that change meanwhile)
+  while (before + v.cost <= z && v.r < p.a.n_req - 1) {   // (z is less than the sum of all: the second bound is for lengths that change meanwhile)
     before += v.cost;
     v.cost = measure<ST>(p, ++v.r, &v.shown, &v.shift);
   }
   v.cost = max(v.cost, 1);
-  const int64_t rest = x - before * p.units;
-  v.u = static_cast<int32_t>(quotient(rest, v.cost));
-  v.step = static_cast<int32_t>(rest - static_cast<int64_t>(v.u) * v.cost);
+  v.step = static_cast<int32_t>(z - before);
   return v;
 }
 
@@ -170,11 +172,16 @@ template <int ST>
 __device__ __forceinline__ void advance(const Params& p, Unit& v) {
   if (++v.step < v.cost) return;
   v.step = 0;
-  if (++v.u < p.units) return;
-  v.u = 0;
+  int32_t skipped = 0;
 #pragma unroll 1
-  do v.cost = v.r < p.a.n_req - 1 ? measure<ST>(p, ++v.r, &v.shown, &v.shift) : 1;
-  while (v.cost == 0);
+  do {
+    if (++v.r == p.a.n_req) {
+      v.r = 0;
+      ++v.u;
+    }
+    v.cost = measure<ST>(p, v.r, &v.shown, &v.shift);
+  } while (v.cost == 0 && ++skipped < p.a.n_req);   // (some request has steps: the bound is for lengths that change meanwhile)
+  v.cost = max(v.cost, 1);
 }
 
 struct Heads {
@@ -238,20 +245,19 @@ __device__ __forceinline__ float join_weight(float& lse) {
 // ---------------------------------------------------------------- the kernel
 // Shared memory: a ring of STAGES steps per warp (at a warp's end also its last piece), the warps' first pieces, the steps' masks
 // and exponents.
-template <int MODE, int D, int NT, bool QBF, int STAGES>
-__global__ void __launch_bounds__(32 * kMaxWarps, 1)
+template <int MODE, int D, int NT, bool QBF>
+__global__ void __launch_bounds__(32 * Shape<MODE, D, NT>::W, 1)
 paged_attention(const __grid_constant__ Params p) {
   using S = Shape<MODE, D, NT>;
-  constexpr int ST = S::ST, PADDED = S::PADDED, ROW = S::ROW;
+  constexpr int ST = S::ST, PADDED = S::PADDED, ROW = S::ROW, W = S::W, THREADS = 32 * W, STAGES = S::STAGES;
   constexpr bool E4 = MODE == WK_E4M3, BF = MODE == WK_BF16;
   constexpr int MT = D / 16;   // row tiles of O^T, and steps along the dimensions in S
   extern __shared__ __align__(1024) uint8_t dyn[];
-  __shared__ int64_t pre[32 * kMaxWarps], parts[kMaxWarps];
-  __shared__ float plse[2 * kMaxWarps][8 * NT];
-  __shared__ Piece piece[2 * kMaxWarps], split[2];
-  __shared__ uint32_t masks[kMaxWarps][STAGES][S::RL];
-  __shared__ int32_t first[2], count[2], n_groups, group_at[2 * kMaxWarps + 1];
-  const int W = blockDim.x >> 5, THREADS = blockDim.x;
+  __shared__ uint32_t pre[THREADS], parts[W];
+  __shared__ float plse[2 * W][8 * NT];
+  __shared__ Piece piece[2 * W], split[2];
+  __shared__ uint32_t masks[W][STAGES][S::RL];
+  __shared__ int32_t first[2], count[2], n_groups, group_at[2 * W + 1];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
   uint8_t* const ring = dyn + warp * (STAGES * kStepBytes);
   uint8_t* const firsts = dyn + W * (STAGES * kStepBytes);
@@ -261,9 +267,9 @@ paged_attention(const __grid_constant__ Params p) {
     return reinterpret_cast<float*>(i & 1 ? dyn + (i >> 1) * (STAGES * kStepBytes) : firsts + (i >> 1) * S::PIECE);
   };
 
-  // ---- the line of steps, and this CTA's and this warp's run of it
+  // ---- the line of steps, and this warp's run of it
   const int per = (p.a.n_req + THREADS - 1) / THREADS;
-  int64_t mine = 0;
+  uint32_t mine = 0;
 #pragma unroll 1
   for (int i = 0; i < per; ++i) {
     const int r = tid * per + i;
@@ -272,73 +278,79 @@ paged_attention(const __grid_constant__ Params p) {
     mine += measure<ST>(p, r, &shown, &shift);
     if (blockIdx.x == 0 && p.a.lens[r] > p.room && p.a.status) atomicOr(p.a.status, WK_DEV_BAD_SLOT);
   }
-  int64_t up = mine;
+  uint32_t up = mine;
 #pragma unroll
   for (int d = 1; d < 32; d <<= 1) {
-    const int64_t o = __shfl_up_sync(0xffffffffu, up, d);
+    const uint32_t o = __shfl_up_sync(0xffffffffu, up, d);
     if (lane >= d) up += o;
   }
   if (lane == 31) parts[warp] = up;
   __syncthreads();
-  int64_t before = 0, all = 0;
-#pragma unroll 4
+  uint32_t before = 0, all = 0;
+#pragma unroll
   for (int w = 0; w < W; ++w) {
     if (w < warp) before += parts[w];
     all += parts[w];
   }
   pre[tid] = before + up - mine;
   __syncthreads();
-  const int64_t total = all * p.units;
-  int64_t chunk = quotient(total + gridDim.x - 1, gridDim.x);
-  if (chunk < W) chunk = W;
+  const int64_t total = static_cast<int64_t>(all) * p.units;
+  const int64_t run = quotient(total + gridDim.x * W - 1, gridDim.x * W), chunk = run * W;
   const int64_t a0 = blockIdx.x * chunk, a1 = min(a0 + chunk, total);
   if (a0 >= total) return;
-  const int64_t run = quotient(a1 - a0 + W - 1, W);
   const int64_t x = a0 + warp * run;
   if (lane < 2) piece[2 * warp + lane].r = -1;
 
   if (x < a1) {
     const int32_t steps = static_cast<int32_t>(min(run, a1 - x));
     uint32_t bad = 0;
-    uint32_t row[S::RL], ex[S::RL];
+    int32_t id[S::RL];             // page ids of the step after the next one to ask for, and places in the page
+    uint32_t off[S::RL], row[S::RL], ex[S::RL];
     uint32_t qf[NT][MT][2];
     float sc[NT][2];               // logit scale of query heads 2c, 2c + 1
     float ref[NT][2], refw[NT][2]; // references of the sum and (8 bits) of the weights
     float sum[NT][2], o[NT][MT][4];
-    Unit cur = locate<ST>(p, pre, per, x), nxt = cur;   // of the step at hand, of the next one to ask for
-    Heads hc = heads_of<NT>(p, cur.u), hn = hc;
+    Unit cur = locate<ST, THREADS>(p, pre, per, all, x), nxt = cur;   // of the step at hand, of the one to look up
+    Heads hc = heads_of<NT>(p, cur.u);
+    int32_t kv_up = hc.kv, kv_ask = hc.kv;   // kv heads of the step to look up, of the one to ask for
     int32_t began = cur.step;
     bool fresh = true;
     const uint32_t ring_at = ptx::smem_u32(ring);
     int slot = 0;
 
 #pragma unroll 1
-    for (int32_t i = -STAGES; i < steps; ++i) {
-      // ---- look up the rows of step i + STAGES, a token per lane (or two)
-      const bool ask = i + STAGES < steps;
+    for (int32_t i = -STAGES - 1; i < steps; ++i) {
+      // ---- step i + STAGES: its page ids have come; rows of its tokens, a token per lane (or two)
+      const bool ask = i >= -STAGES && i + STAGES < steps;
       if (ask) {
-        if (i > -STAGES) {
+        kv_ask = kv_up;
+#pragma unroll
+        for (int k = 0; k < S::RL; ++k) {
+          const bool there = static_cast<uint32_t>(id[k]) < static_cast<uint32_t>(p.a.c.n_pages);
+          if (!there && id[k] != -1) bad = WK_DEV_BAD_SLOT;
+          row[k] = there ? id[k] * p.page16 + off[k] * p.token16 : kNowhere;
+          ex[k] = 0;
+          if (E4 && there) {
+            const int64_t e = (static_cast<int64_t>(id[k]) * p.a.c.n_kv_heads + kv_ask) * p.a.c.page_tokens + off[k];
+            ex[k] = __ldg(p.a.c.K_exp + e) | static_cast<uint32_t>(__ldg(p.a.c.V_exp + e)) << 8;
+          }
+        }
+      }
+      // ---- step i + STAGES + 1: look up the page ids
+      if (i + STAGES + 1 < steps) {
+        if (i > -STAGES - 1) {
           advance<ST>(p, nxt);
-          if (nxt.step == 0) hn = heads_of<NT>(p, nxt.u);
+          if (nxt.step == 0) kv_up = heads_of<NT>(p, nxt.u).kv;
         }
 #pragma unroll
         for (int k = 0; k < S::RL; ++k) {
           const int32_t j = nxt.step * ST + (lane & (ST - 1)) + 32 * k;
-          row[k] = kNowhere;
-          ex[k] = 0;
+          id[k] = -1;
           if (j < nxt.shown) {
             const uint32_t pos = static_cast<uint32_t>(j >= p.a.sink ? j + nxt.shift : j);
-            const uint32_t at = pos / static_cast<uint32_t>(p.a.c.page_tokens), off = pos - at * p.a.c.page_tokens;
-            const int32_t id = __ldg(p.a.tables + nxt.r * p.a.table_stride + at);
-            if (id >= 0 && id < p.a.c.n_pages) {
-              row[k] = id * p.page16 + off * p.token16;
-              if (E4) {
-                const int64_t e = (static_cast<int64_t>(id) * p.a.c.n_kv_heads + hn.kv) * p.a.c.page_tokens + off;
-                ex[k] = __ldg(p.a.c.K_exp + e) | static_cast<uint32_t>(__ldg(p.a.c.V_exp + e)) << 8;
-              }
-            } else if (id != -1) {
-              bad = WK_DEV_BAD_SLOT;
-            }
+            const uint32_t at = pos / static_cast<uint32_t>(p.a.c.page_tokens);
+            off[k] = pos - at * p.a.c.page_tokens;
+            id[k] = __ldg(p.a.tables + nxt.r * p.a.table_stride + at);
           }
         }
       }
@@ -521,8 +533,8 @@ paged_attention(const __grid_constant__ Params p) {
       __syncwarp();
       if (ask) {
         const uint32_t to = ring_at + slot * kStepBytes;
-        const char* const kb = static_cast<const char*>(p.a.c.K) + hn.kv * p.head_bytes + lane % S::LPR * 16;
-        const char* const vb = static_cast<const char*>(p.a.c.V) + hn.kv * p.head_bytes + lane % S::LPR * 16;
+        const char* const kb = static_cast<const char*>(p.a.c.K) + kv_ask * p.head_bytes + lane % S::LPR * 16;
+        const char* const vb = static_cast<const char*>(p.a.c.V) + kv_ask * p.head_bytes + lane % S::LPR * 16;
         const uint32_t chunk = lane % S::LPR;
 #pragma unroll 2
         for (int k = 0; k < 8; ++k) {
@@ -639,7 +651,7 @@ paged_attention(const __grid_constant__ Params p) {
   // ---- pieces of one unit lie next to each other: joined into O, or into this CTA's piece.  A warp takes a row at a time.
   float* const partial = reinterpret_cast<float*>(p.a.scratch + p.counter_bytes);
   if (warp == 0) {
-    static_assert(2 * kMaxWarps <= 32, "a lane per piece");
+    static_assert(2 * W <= 32, "a lane per piece");
     const bool there = lane < 2 * W && piece[lane].r >= 0;
     const uint32_t below = __ballot_sync(0xffffffffu, there) & ((1u << lane) - 1);
     const int prev = below ? 31 - __clz(below) : lane;
@@ -650,8 +662,12 @@ paged_attention(const __grid_constant__ Params p) {
     if (start) {
       const Piece u = piece[lane];
       group_at[__popc(starts & ((1u << lane) - 1))] = lane;
-      if (u.start < a0) split[0] = u;
-      else if (u.start + u.cost > a1) split[1] = u;
+      if (u.start < a0 || u.start + u.cost > a1) {
+        const int side = u.start < a0 ? 0 : 1;
+        split[side] = u;
+        first[side] = static_cast<int>(quotient(u.start, chunk));
+        count[side] = static_cast<int>(quotient(u.start + u.cost - 1, chunk)) - first[side] + 1;
+      }
     }
     if (lane == 0) {
       n_groups = __popc(starts);
@@ -692,14 +708,14 @@ paged_attention(const __grid_constant__ Params p) {
   // ---- units that other CTAs share: the last of them to arrive joins the pieces
   __syncthreads();
   if (tid < 2) {
-    count[tid] = 0;
-    if (split[tid].r >= 0) {
-      first[tid] = static_cast<int>(quotient(split[tid].start, chunk));
-      const uint32_t n = static_cast<uint32_t>(quotient(split[tid].start + split[tid].cost - 1, chunk)) - first[tid];
+    const uint32_t n = split[tid].r < 0 ? 0 : count[tid] - 1;
+    bool mine = false;
+    if (n) {
       __threadfence();   // the barrier has ordered the CTA's pieces before this
-      if (atomicInc(reinterpret_cast<uint32_t*>(p.a.scratch) + first[tid], n) == n) count[tid] = n + 1;
+      mine = atomicInc(reinterpret_cast<uint32_t*>(p.a.scratch) + first[tid], n) == n;
       __threadfence();
     }
+    if (!mine) count[tid] = 0;
   }
   __syncthreads();
   Vec* const part = reinterpret_cast<Vec*>(dyn);   // [W][32]
@@ -766,24 +782,23 @@ paged_attention(const __grid_constant__ Params p) {
   }
 }
 
-template <int MODE, int D, int NT, bool QBF, int STAGES>
-wk_status launch(wk_ctx* ctx, const Params& p, int warps, cudaStream_t s) {
+template <int MODE, int D, int NT, bool QBF>
+wk_status launch(wk_ctx* ctx, const Params& p, cudaStream_t s) {
   using S = Shape<MODE, D, NT>;
-  const int smem = warps * (STAGES * kStepBytes + S::PIECE + STAGES * S::META);
+  constexpr int smem = S::W * (S::STAGES * (kStepBytes + S::META) + S::PIECE);
   const int i = ((MODE * 2 + (D == 128)) * 2 + NT - 1) * 2 + QBF;
-  if (ctx->paged_smem[i] < smem) {
-    WK_CUDA_TRY(ctx, cudaFuncSetAttribute(paged_attention<MODE, D, NT, QBF, STAGES>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-    ctx->paged_smem[i] = smem;
+  if (!(ctx->paged_attr_set >> i & 1)) {
+    WK_CUDA_TRY(ctx, cudaFuncSetAttribute(paged_attention<MODE, D, NT, QBF>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+    ctx->paged_attr_set |= 1u << i;
   }
-  paged_attention<MODE, D, NT, QBF, STAGES><<<ctx->sm_count, 32 * warps, smem, s>>>(p);
+  paged_attention<MODE, D, NT, QBF><<<ctx->sm_count, 32 * S::W, smem, s>>>(p);
   return after_launch(ctx);
 }
 
 template <int MODE, bool QBF>
 wk_status choose(wk_ctx* ctx, const Params& p, int nt, cudaStream_t s) {
-  const int warps = nt == 1 ? 10 : 8;
-  if (p.a.c.head_dim == 128) return nt == 1 ? launch<MODE, 128, 1, QBF, 2>(ctx, p, warps, s) : launch<MODE, 128, 2, QBF, 2>(ctx, p, warps, s);
-  return nt == 1 ? launch<MODE, 64, 1, QBF, 2>(ctx, p, warps, s) : launch<MODE, 64, 2, QBF, 2>(ctx, p, warps, s);
+  if (p.a.c.head_dim == 128) return nt == 1 ? launch<MODE, 128, 1, QBF>(ctx, p, s) : launch<MODE, 128, 2, QBF>(ctx, p, s);
+  return nt == 1 ? launch<MODE, 64, 1, QBF>(ctx, p, s) : launch<MODE, 64, 2, QBF>(ctx, p, s);
 }
 
 }  // namespace
