@@ -424,21 +424,28 @@ class PagedKV:
                   starts_out: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
         """Pages and slots for the next step's tokens; lens and state are advanced in place unless lens_out, state_out are
         given.  Returns (slots [max_tokens], starts [n_req + 1]) int32, on the device."""
-        n = lens.size(0)
-        lens_out = lens if lens_out is None else lens_out
-        state_out = state if state_out is None else state_out
+        dev, n = self._index, lens.numel()
+        if lens_out is None:
+            lens_out = lens
+        elif not _ints(lens_out, n, dev):
+            raise WkError(WK_ERR_ARG, "wk_page_plan: lens_out [n_req] int32")
+        if state_out is None:
+            state_out = state
+        elif not _ints(state_out, 4, dev):
+            raise WkError(WK_ERR_ARG, "wk_page_plan: state_out [4] int32")
+        if not (_ints(lens, n, dev) and _ints(new_tokens, n, dev) and _ints(ring, self.n_pages, dev) and _ints(state, 4, dev)):
+            raise WkError(WK_ERR_ARG, "wk_page_plan: lens, new_tokens [n_req], ring [n_pages], state [4] int32, on the context's device")
+        rows, max_pages = _table(tables, n, dev, "wk_page_plan")
         if slots_out is None:
-            slots_out = torch.empty(max_tokens, dtype=torch.int32, device=self.device)
+            slots_out = lens.new_empty(max_tokens)
+        elif not _ints(slots_out, max_tokens, dev):
+            raise WkError(WK_ERR_ARG, "wk_page_plan: slots_out [max_tokens] int32")
         if starts_out is None:
-            starts_out = torch.empty(n + 1, dtype=torch.int32, device=self.device)
-        for x, size in ((lens, n), (new_tokens, n), (lens_out, n), (ring, self.n_pages), (state, 4), (state_out, 4),
-                        (slots_out, max_tokens), (starts_out, n + 1)):
-            _need(x.dtype == torch.int32 and x.dim() == 1 and x.size(0) >= size and x.is_contiguous()
-                  and x.get_device() == self._index, "wk_page_plan: int32 arrays of the right length on the context's device")
-        _need(tables.dtype == torch.int32 and tables.dim() == 2 and tables.size(0) >= n and tables.stride(1) == 1
-              and tables.get_device() == self._index, "wk_page_plan: tables [n_req, max_pages] int32")
+            starts_out = lens.new_empty(n + 1)
+        elif not _ints(starts_out, n + 1, dev):
+            raise WkError(WK_ERR_ARG, "wk_page_plan: starts_out [n_req + 1] int32")
         st = self.lib.wk_page_plan(self.kv.ctx, self.n_pages, self.page_tokens, n, lens.data_ptr(), new_tokens.data_ptr(),
-                                   lens_out.data_ptr(), tables.data_ptr(), tables.size(1), tables.stride(0), ring.data_ptr(),
+                                   lens_out.data_ptr(), tables.data_ptr(), max_pages, rows, ring.data_ptr(),
                                    state.data_ptr(), state_out.data_ptr(), max_tokens, slots_out.data_ptr(),
                                    starts_out.data_ptr(), self._stream(stream))
         if st != WK_OK:
@@ -447,16 +454,16 @@ class PagedKV:
 
     def page_store(self, K_new: torch.Tensor, V_new: torch.Tensor, slots: torch.Tensor, stream=None) -> None:
         """Rows K_new, V_new [n, n_kv_heads, head_dim] (heads contiguous, any row stride, both alike) into slots [>= n]."""
-        n = K_new.size(0)
-        row = (self.n_kv_heads, self.head_dim)
-        _need(self._desc is not None and K_new.shape == V_new.shape and K_new.shape[1:] == row and K_new.dtype == V_new.dtype
-              and K_new.dtype in _TYPES and K_new.stride() == V_new.stride() and _rows(K_new) and K_new.get_device() == self._index
-              and V_new.get_device() == self._index,
-              "wk_page_store: K_new, V_new [n, n_kv_heads, head_dim] alike, heads contiguous")
-        _need(slots.dtype == torch.int32 and slots.dim() == 1 and slots.size(0) >= n and slots.is_contiguous()
-              and slots.get_device() == self._index, "wk_page_store: slots int32")
-        st = self.lib.wk_page_store(self.kv.ctx, self._desc_at, K_new.data_ptr(), V_new.data_ptr(), _TYPES[K_new.dtype], n,
-                                    K_new.stride(0), slots.data_ptr(), self._stream(stream))
+        dev, shape, strides, dtype = self._index, K_new.shape, K_new.stride(), K_new.dtype
+        if not (self._desc is not None and len(shape) == 3 and shape[1] == self.n_kv_heads and shape[2] == self.head_dim
+                and V_new.shape == shape and V_new.stride() == strides and V_new.dtype is dtype and dtype in _TYPES
+                and strides[2] == 1 and (strides[1] == shape[2] or shape[1] == 1)
+                and K_new.get_device() == dev and V_new.get_device() == dev):
+            raise WkError(WK_ERR_ARG, "wk_page_store: K_new, V_new [n, n_kv_heads, head_dim] alike, heads contiguous")
+        if not _ints(slots, shape[0], dev):
+            raise WkError(WK_ERR_ARG, "wk_page_store: slots int32")
+        st = self.lib.wk_page_store(self.kv.ctx, self._desc_at, K_new.data_ptr(), V_new.data_ptr(), _TYPES[dtype], shape[0],
+                                    strides[0], slots.data_ptr(), self._stream(stream))
         if st != WK_OK:
             raise WkError(st, "wk_page_store")
 
@@ -466,29 +473,28 @@ class PagedKV:
         """O [n_req, n_heads, head_dim] of one new token per request: Q [n_req, n_heads, head_dim] (heads contiguous, any
         row stride) over the tokens that tables and lens name.  scratch: as WorldKV's, shared by the calls of a context unless
         given (zero-filled once; for calls that may overlap on the GPU)."""
-        n, heads, d = Q.shape
+        dev, shape, strides, dtype = self._index, Q.shape, Q.stride(), Q.dtype
+        if not (self._desc is not None and len(shape) == 3 and shape[2] == self.head_dim and dtype in _TYPES and strides[2] == 1
+                and (strides[1] == shape[2] or shape[1] == 1) and Q.get_device() == dev):
+            raise WkError(WK_ERR_ARG, "wk_paged_attention: Q [n_req, n_heads, head_dim], heads contiguous")
+        n, heads, d = shape
+        if not _ints(lens, n, dev):
+            raise WkError(WK_ERR_ARG, "wk_paged_attention: lens [n_req] int32")
+        rows, max_pages = _table(tables, n, dev, "wk_paged_attention")
+        if O is None:
+            O = torch.empty_like(Q) if Q.is_contiguous() else Q.new_empty(shape)
+        elif not (O.shape == shape and O.dtype is dtype and O.is_contiguous() and O.get_device() == dev):
+            raise WkError(WK_ERR_ARG, "wk_paged_attention: O like Q, contiguous")
+        if lse_out is not None and not (lse_out.shape == shape[:2] and lse_out.dtype is torch.float32
+                                        and lse_out.is_contiguous() and lse_out.get_device() == dev):
+            raise WkError(WK_ERR_ARG, "wk_paged_attention: lse_out [n_req, n_heads] fp32")
         if scratch is None:
             scratch = self.kv.paged_scratch
-        _need(self._desc is not None and d == self.head_dim and Q.dtype in _TYPES and _rows(Q) and Q.get_device() == self._index,
-              "wk_paged_attention: Q [n_req, n_heads, head_dim], heads contiguous")
-        _need(tables.dtype == torch.int32 and tables.dim() == 2 and tables.size(0) >= n and tables.stride(1) == 1
-              and tables.get_device() == self._index and lens.dtype == torch.int32 and lens.dim() == 1 and lens.size(0) >= n
-              and lens.is_contiguous() and lens.get_device() == self._index,
-              "wk_paged_attention: tables [n_req, max_pages] and lens [n_req] int32")
-        if O is None:
-            O = torch.empty((n, heads, d), dtype=Q.dtype, device=self.device)
-        else:
-            _need(O.shape == Q.shape and O.dtype == Q.dtype and O.is_contiguous() and O.get_device() == self._index,
-                  "wk_paged_attention: O like Q, contiguous")
-        if lse_out is not None:
-            _need(lse_out.shape == (n, heads) and lse_out.dtype == torch.float32 and lse_out.is_contiguous()
-                  and lse_out.get_device() == self._index, "wk_paged_attention: lse_out [n_req, n_heads] fp32")
         if n == 0:
             return O
-        st = self.lib.wk_paged_attention(self.kv.ctx, self._desc_at, Q.data_ptr(), _TYPES[Q.dtype], Q.stride(0), n, heads,
-                                         tables.data_ptr(), tables.size(1), tables.stride(0), lens.data_ptr(), window, sink,
-                                         softmax_scale, O.data_ptr(), _ptr(lse_out), scratch.data_ptr(), scratch.numel(),
-                                         self._stream(stream))
+        st = self.lib.wk_paged_attention(self.kv.ctx, self._desc_at, Q.data_ptr(), _TYPES[dtype], strides[0], n, heads,
+                                         tables.data_ptr(), max_pages, rows, lens.data_ptr(), window, sink, softmax_scale,
+                                         O.data_ptr(), _ptr(lse_out), scratch.data_ptr(), scratch.numel(), self._stream(stream))
         if st != WK_OK:
             raise WkError(st, f"wk_paged_attention (last CUDA error {self.kv.last_cuda_error()})")
         return O
@@ -499,6 +505,13 @@ def _need(ok: bool, what: str) -> None:
         raise WkError(WK_ERR_ARG, what)
 
 
-def _rows(x: torch.Tensor) -> bool:
-    """Rows [n, heads, head_dim] whose heads lie one after the other."""
-    return x.stride(2) == 1 and (x.size(1) == 1 or x.stride(1) == x.size(2))
+def _ints(x: torch.Tensor, size: int, device: int) -> bool:
+    return x.dtype is torch.int32 and x.numel() >= size and x.is_contiguous() and x.get_device() == device
+
+
+def _table(tables: torch.Tensor, n: int, device: int, what: str) -> Tuple[int, int]:
+    """(row stride, columns) of block tables [>= n, max_pages]."""
+    shape, strides = tables.shape, tables.stride()
+    if not (tables.dtype is torch.int32 and len(shape) == 2 and shape[0] >= n and strides[1] == 1 and tables.get_device() == device):
+        raise WkError(WK_ERR_ARG, what + ": tables [n_req, max_pages] int32")
+    return strides[0], shape[1]

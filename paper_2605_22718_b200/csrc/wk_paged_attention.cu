@@ -43,13 +43,14 @@ struct Params {
   uint32_t page16, token16;        // strides in units of 16 bytes
   int64_t head_bytes;              // stride of a kv head
   int32_t counter_bytes;           // of the scratch buffer, before the pieces
+  uint32_t page_mul, page_shift;   // pos / page_tokens = pos * page_mul >> page_shift for pos < 2^31
 };
 
 template <int MODE, int D, int NT>
 struct Shape {
-  // Warps: as few as keep the memory busy, for fewer copies in flight are served more evenly (8: 203 us for 1.35 GB, 10: 213), and
-  // as many as the ring leaves room for where arithmetic counts too (8 bits: 6 warps 275 us for 0.92 GB, 8: 224, 10: 198).
-  static constexpr int W = MODE == WK_E4M3 && NT == 1 ? 10 : 8;
+  // As many warps as keep the memory busy, and no more: with fewer copies in flight the SMs are served more evenly (1.35 GB in
+  // bf16: 6 warps 230 us, 7 207, 8 204, 10 211; with a third step in the ring 218.  0.92 GB in 8 bits: 7 170, 8 174, 10 188).
+  static constexpr int W = 8;
   static constexpr int STAGES = 2;
   static constexpr int ES = MODE == WK_E4M3 ? 1 : 2;     // bytes per element of the cache
   static constexpr int ROW = D * ES;                     // bytes of a row
@@ -59,7 +60,7 @@ struct Shape {
   static constexpr int RPI = 32 / LPR;                   // rows per copy instruction
   static constexpr int PADDED = D + 4;
   static constexpr int PIECE = 8 * NT * PADDED * 4;      // bytes of a piece in shared memory
-  static constexpr int META = MODE == WK_E4M3 ? 2 * ST : 0;   // exponents of a step's tokens
+  static constexpr int META = MODE == WK_E4M3 ? 2 * ST : 0;   // bytes of a step's exponents, K's and V's side by side
 };
 
 // ---------------------------------------------------------------- instructions
@@ -124,7 +125,7 @@ using ptx::ex2_approx;
 // The line: for every unit of a request (kv heads first) the steps of all requests, one after the other.
 struct Unit {
   int32_t r, u;         // request, unit of the request
-  int32_t step, cost;   // place in the unit, steps of the unit (at least one, also where nothing is visible)
+  int32_t cost, left;   // steps of the unit (at least one, also where nothing is visible), those from the one at hand on
   int32_t shown, shift; // visible tokens; visible token j is position j, or j + shift from the sink's end on
 };
 
@@ -164,14 +165,13 @@ __device__ __forceinline__ Unit locate(const Params& p, const uint32_t* pre, int
     v.cost = measure<ST>(p, ++v.r, &v.shown, &v.shift);
   }
   v.cost = max(v.cost, 1);
-  v.step = static_cast<int32_t>(z - before);
+  v.left = v.cost - static_cast<int32_t>(z - before);
   return v;
 }
 
+// The unit behind v on the line.
 template <int ST>
-__device__ __forceinline__ void advance(const Params& p, Unit& v) {
-  if (++v.step < v.cost) return;
-  v.step = 0;
+__device__ __forceinline__ void next_unit(const Params& p, Unit& v) {
   int32_t skipped = 0;
 #pragma unroll 1
   do {
@@ -181,7 +181,7 @@ __device__ __forceinline__ void advance(const Params& p, Unit& v) {
     }
     v.cost = measure<ST>(p, v.r, &v.shown, &v.shift);
   } while (v.cost == 0 && ++skipped < p.a.n_req);   // (some request has steps: the bound is for lengths that change meanwhile)
-  v.cost = max(v.cost, 1);
+  v.left = v.cost = max(v.cost, 1);
 }
 
 struct Heads {
@@ -261,7 +261,7 @@ paged_attention(const __grid_constant__ Params p) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
   uint8_t* const ring = dyn + warp * (STAGES * kStepBytes);
   uint8_t* const firsts = dyn + W * (STAGES * kStepBytes);
-  uint16_t* const exps = reinterpret_cast<uint16_t*>(firsts + W * S::PIECE) + warp * (STAGES * ST);
+  uint8_t* const exps = firsts + W * S::PIECE + warp * (STAGES * S::META);
   // piece i of the CTA (warp i / 2's first or last)
   auto piece_rows = [&](int i) -> float* {
     return reinterpret_cast<float*>(i & 1 ? dyn + (i >> 1) * (STAGES * kStepBytes) : firsts + (i >> 1) * S::PIECE);
@@ -305,7 +305,7 @@ paged_attention(const __grid_constant__ Params p) {
     const int32_t steps = static_cast<int32_t>(min(run, a1 - x));
     uint32_t bad = 0;
     int32_t id[S::RL];             // page ids of the step after the next one to ask for, and places in the page
-    uint32_t off[S::RL], row[S::RL], ex[S::RL];
+    uint32_t off[S::RL], row[S::RL], kx[S::RL], vx[S::RL];
     uint32_t qf[NT][MT][2];
     float sc[NT][2];               // logit scale of query heads 2c, 2c + 1
     float ref[NT][2], refw[NT][2]; // references of the sum and (8 bits) of the weights
@@ -313,15 +313,30 @@ paged_attention(const __grid_constant__ Params p) {
     Unit cur = locate<ST, THREADS>(p, pre, per, all, x), nxt = cur;   // of the step at hand, of the one to look up
     Heads hc = heads_of<NT>(p, cur.u);
     int32_t kv_up = hc.kv, kv_ask = hc.kv;   // kv heads of the step to look up, of the one to ask for
-    int32_t began = cur.step;
+    int32_t j_up = (cur.cost - cur.left) * ST + (lane & (ST - 1));   // this lane's token of the step to look up
+    const int32_t* table = p.a.tables + cur.r * p.a.table_stride;
+    bool whole = cur.left == cur.cost;       // the unit at hand began in this run
     bool fresh = true;
-    const uint32_t ring_at = ptx::smem_u32(ring);
+    // Where this lane's chunks go: token k * RPI + lane / LPR, swizzled so that eight rows' chunks lie in different banks.
+    const uint32_t ring_at = ptx::smem_u32(ring), chunk_l = lane % S::LPR, hi = lane / S::LPR;
+    const uint32_t to_l = hi * ROW + ((chunk_l ^ (ROW == 64 ? hi >> 1 & 3 : hi)) << 4);
+    const int64_t v_minus_k = static_cast<const char*>(p.a.c.V) - static_cast<const char*>(p.a.c.K);
     int slot = 0;
 
 #pragma unroll 1
     for (int32_t i = -STAGES - 1; i < steps; ++i) {
       // ---- step i + STAGES: its page ids have come; rows of its tokens, a token per lane (or two)
       const bool ask = i >= -STAGES && i + STAGES < steps;
+      if constexpr (E4) {   // the exponents of the step asked for last have come, too
+        if (i > -STAGES && i + STAGES <= steps) {
+          uint8_t* const to = exps + (slot ? slot - 1 : STAGES - 1) * S::META + 2 * (lane & (ST - 1));
+#pragma unroll
+          for (int k = 0; k < S::RL; ++k) {
+            to[64 * k] = static_cast<uint8_t>(kx[k]);
+            to[64 * k + 1] = static_cast<uint8_t>(vx[k]);
+          }
+        }
+      }
       if (ask) {
         kv_ask = kv_up;
 #pragma unroll
@@ -329,28 +344,33 @@ paged_attention(const __grid_constant__ Params p) {
           const bool there = static_cast<uint32_t>(id[k]) < static_cast<uint32_t>(p.a.c.n_pages);
           if (!there && id[k] != -1) bad = WK_DEV_BAD_SLOT;
           row[k] = there ? id[k] * p.page16 + off[k] * p.token16 : kNowhere;
-          ex[k] = 0;
-          if (E4 && there) {
-            const int64_t e = (static_cast<int64_t>(id[k]) * p.a.c.n_kv_heads + kv_ask) * p.a.c.page_tokens + off[k];
-            ex[k] = __ldg(p.a.c.K_exp + e) | static_cast<uint32_t>(__ldg(p.a.c.V_exp + e)) << 8;
+          if constexpr (E4) {
+            const int64_t e = there ? (static_cast<int64_t>(id[k]) * p.a.c.n_kv_heads + kv_ask) * p.a.c.page_tokens + off[k] : 0;
+            kx[k] = __ldg(p.a.c.K_exp + e);   // (of any token where there is none)
+            vx[k] = __ldg(p.a.c.V_exp + e);
           }
         }
       }
       // ---- step i + STAGES + 1: look up the page ids
       if (i + STAGES + 1 < steps) {
         if (i > -STAGES - 1) {
-          advance<ST>(p, nxt);
-          if (nxt.step == 0) kv_up = heads_of<NT>(p, nxt.u).kv;
+          j_up += ST;
+          if (--nxt.left == 0) {
+            next_unit<ST>(p, nxt);
+            kv_up = heads_of<NT>(p, nxt.u).kv;
+            j_up = lane & (ST - 1);
+            table = p.a.tables + nxt.r * p.a.table_stride;
+          }
         }
 #pragma unroll
         for (int k = 0; k < S::RL; ++k) {
-          const int32_t j = nxt.step * ST + (lane & (ST - 1)) + 32 * k;
+          const int32_t j = j_up + 32 * k;
           id[k] = -1;
           if (j < nxt.shown) {
             const uint32_t pos = static_cast<uint32_t>(j >= p.a.sink ? j + nxt.shift : j);
-            const uint32_t at = pos / static_cast<uint32_t>(p.a.c.page_tokens);
+            const uint32_t at = static_cast<uint32_t>(static_cast<uint64_t>(pos) * p.page_mul >> p.page_shift);
             off[k] = pos - at * p.a.c.page_tokens;
-            id[k] = __ldg(p.a.tables + nxt.r * p.a.table_stride + at);
+            id[k] = __ldg(table + at);
           }
         }
       }
@@ -405,14 +425,18 @@ paged_attention(const __grid_constant__ Params p) {
         {
           const int r8 = lane & 7, sw = ROW == 64 ? r8 >> 1 : r8;
           const uint32_t at = k_at + ((lane >> 3 & 1) * 8 + r8) * ROW + (((lane >> 4) ^ sw) << 4);
+          constexpr int CHAINS = ST == 16 ? 2 : 1;   // sums that do not wait for one another (steps of several tiles have them anyway)
+          float more[ST / 16][NT][4];
 #pragma unroll
-          for (int t = 0; t < ST / 16; ++t) {
+          for (int t = 0; t < ST / 16; ++t)
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-              for (int e = 0; e < 4; ++e) s[t][nt][e] = 0.f;
+              for (int e = 0; e < 4; ++e) s[t][nt][e] = more[t][nt][e] = 0.f;
 #pragma unroll
-            for (int j = 0; j < ROW / 32; ++j) {
+          for (int j = 0; j < ROW / 32; ++j)
+#pragma unroll
+            for (int t = 0; t < ST / 16; ++t) {
               uint32_t f[4];
               load_matrices<false>(f, (at + t * 16 * ROW) ^ (j << 5));
               if constexpr (E4) {
@@ -424,9 +448,15 @@ paged_attention(const __grid_constant__ Params p) {
                 }
               } else {
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt) mma<BF>(s[t][nt], f[0], f[1], f[2], f[3], qf[nt][j][0], qf[nt][j][1]);
+                for (int nt = 0; nt < NT; ++nt)
+                  mma<BF>(CHAINS == 2 && j % 2 ? more[t][nt] : s[t][nt], f[0], f[1], f[2], f[3], qf[nt][j][0], qf[nt][j][1]);
               }
             }
+          if (CHAINS == 2) {
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) s[0][nt][e] += more[0][nt][e];
           }
         }
         // ---- logits (log2), their largest, the references
@@ -435,23 +465,41 @@ paged_attention(const __grid_constant__ Params p) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) top[nt][0] = top[nt][1] = topw[nt][0] = topw[nt][1] = -INFINITY;
 #pragma unroll
-        for (int t = 0; t < ST / 16; ++t) {
-          const uint32_t mask = masks[warp][slot][t / 2] >> (t % 2 * 16 + g);
+        for (int t = 0; t < ST / 16; ++t)
 #pragma unroll
           for (int hh = 0; hh < 2; ++hh) {
-            const bool on = mask >> (8 * hh) & 1;
-            float kscale = 1.f, vpower = 0.f;
-            if (E4) {
-              const uint32_t e = exps[slot * ST + t * 16 + hh * 8 + g];
-              kscale = __uint_as_float((e & 255u) << 23);
-              vpower = static_cast<float>(static_cast<int>(e >> 8) - 127);
-            }
+            float kscale = 1.f;
+            if constexpr (E4) kscale = __uint_as_float(static_cast<uint32_t>(exps[slot * S::META + 2 * (t * 16 + hh * 8 + g)]) << 23);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int e = 0; e < 2; ++e) s[t][nt][2 * hh + e] *= E4 ? sc[nt][e] * kscale : sc[nt][e];
+          }
+#pragma unroll
+        for (int k = 0; k < S::RL; ++k) {
+          const uint32_t mask = masks[warp][slot][k];
+          if (mask != 0xffffffffu) {
+#pragma unroll
+            for (int t = 2 * k; t < (ST == 16 ? 1 : 2 * k + 2); ++t)
+#pragma unroll
+              for (int hh = 0; hh < 2; ++hh)
+                if (!(mask >> (t % 2 * 16 + hh * 8 + g) & 1)) {
+#pragma unroll
+                  for (int nt = 0; nt < NT; ++nt) s[t][nt][2 * hh] = s[t][nt][2 * hh + 1] = -INFINITY;
+                }
+          }
+        }
+#pragma unroll
+        for (int t = 0; t < ST / 16; ++t)
+#pragma unroll
+          for (int hh = 0; hh < 2; ++hh) {
+            float vpower = 0.f;
+            if constexpr (E4) vpower = static_cast<float>(static_cast<int>(exps[slot * S::META + 2 * (t * 16 + hh * 8 + g) + 1]) - 127);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
               for (int e = 0; e < 2; ++e) {
-                float& v = s[t][nt][2 * hh + e];
-                v = on ? v * (E4 ? sc[nt][e] * kscale : sc[nt][e]) : -INFINITY;
+                const float v = s[t][nt][2 * hh + e];
                 top[nt][e] = fmaxf(top[nt][e], v);
                 if constexpr (E4) {
                   w[t][nt][2 * hh + e] = v + vpower;
@@ -459,7 +507,6 @@ paged_attention(const __grid_constant__ Params p) {
                 }
               }
           }
-        }
         bool moved = false;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -532,37 +579,35 @@ paged_attention(const __grid_constant__ Params p) {
       // ---- ask for the rows just looked up, in the place of the step just used
       __syncwarp();
       if (ask) {
-        const uint32_t to = ring_at + slot * kStepBytes;
-        const char* const kb = static_cast<const char*>(p.a.c.K) + kv_ask * p.head_bytes + lane % S::LPR * 16;
-        const char* const vb = static_cast<const char*>(p.a.c.V) + kv_ask * p.head_bytes + lane % S::LPR * 16;
-        const uint32_t chunk = lane % S::LPR;
-#pragma unroll 2
+        const uint32_t to = ring_at + slot * kStepBytes + to_l;
+        const char* const from = static_cast<const char*>(p.a.c.K) + kv_ask * p.head_bytes + chunk_l * 16;
+#pragma unroll
         for (int k = 0; k < 8; ++k) {
-          const int token = k * S::RPI + lane / S::LPR;
-          const uint32_t at = __shfl_sync(0xffffffffu, S::RL == 1 || k < 4 ? row[0] : row[S::RL - 1], token & 31);
-          const uint32_t skip = at == kNowhere;
-          const uint64_t src = static_cast<uint64_t>(skip ? 0 : at) * 16;
-          const uint32_t dst = to + token * ROW + ((chunk ^ (ROW == 64 ? token >> 1 & 3 : token & 7)) << 4);
-          copy16(dst, kb + src, skip);
-          copy16(dst + kStepBytes / 2, vb + src, skip);
+          const uint32_t at = __shfl_sync(0xffffffffu, row[S::RL == 1 || k < 4 ? 0 : S::RL - 1], (k * S::RPI + hi) & 31);
+          const bool skip = at == kNowhere;
+          const char* const src = from + static_cast<uint64_t>(skip ? 0 : at) * 16;
+          const uint32_t dst = (ROW == 64 ? to : to ^ ((k * S::RPI & 7) << 4)) + k * 512;
+          copy16(dst, src, skip);
+          copy16(dst + kStepBytes / 2, src + v_minus_k, skip);
         }
 #pragma unroll
         for (int k = 0; k < S::RL; ++k) {
           const uint32_t mask = __ballot_sync(0xffffffffu, row[k] != kNowhere);
           if (lane == 0) masks[warp][slot][k] = mask;
-          if (E4) exps[slot * ST + (lane & (ST - 1)) + 32 * k] = static_cast<uint16_t>(ex[k]);
         }
       }
       copies_commit();
       if (++slot == STAGES) slot = 0;
 
       // ---- does the unit end here, or this warp's part of it?
-      const bool ends = i >= 0 && (i + 1 == steps || cur.step + 1 == cur.cost);
+      if (i < -1) continue;
+      const bool over = i >= 0 && --cur.left == 0, ends = over || i + 1 == steps;
+      if (!ends && i >= 0) continue;
       const Unit was = cur;
       const Heads hw = hc;
-      if (i >= 0 && i + 1 < steps) {
-        advance<ST>(p, cur);
-        if (ends) hc = heads_of<NT>(p, cur.u);
+      if (over && i + 1 < steps) {
+        next_unit<ST>(p, cur);
+        hc = heads_of<NT>(p, cur.u);
       }
       float f[NT][2];
       if (ends) {
@@ -577,7 +622,7 @@ paged_attention(const __grid_constant__ Params p) {
             f[nt][e] = l == 0.f ? 0.f : __fdividef(E4 ? ex2_approx(refw[nt][e] - ref[nt][e]) : 1.f, l);
           }
       }
-      if (ends ? i + 1 < steps : i == -1) {   // Q of the unit that comes next: row g of every tile
+      if (i + 1 < steps) {   // Q of the unit that comes next: row g of every tile
         fresh = true;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -597,10 +642,8 @@ paged_attention(const __grid_constant__ Params p) {
         }
       }
       if (ends) {
-        const bool whole = began == 0 && was.step + 1 == was.cost;
-        const int which = 2 * warp + (began == 0);   // reaches in: the warp's first unit; out: its last
-        began = 0;
-        if (whole) {
+        const int which = 2 * warp + whole;   // reaches in: the warp's first unit; out: its last
+        if (whole && over) {
           // transposed in registers: lane (g, c) then has head g's dimensions 2c, 2c + 1 of every 8 (8 bits: 4c .. 4c + 3 of 16)
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
@@ -640,8 +683,9 @@ paged_attention(const __grid_constant__ Params p) {
                   rows[q * PADDED + m * 16 + (E4 ? 2 * g + h : 8 * h + g)] = o[nt][m][2 * h + e] * f[nt][e];
               if (g == 0) plse[which][q] = sum[nt][e];
             }
-          if (lane == 0) piece[which] = Piece{was.r, was.u, was.cost, x + i - was.step};
+          if (lane == 0) piece[which] = Piece{was.r, was.u, was.cost, x + i + 1 - (was.cost - was.left)};
         }
+        whole = true;
       }
     }
     if (bad && p.a.status) atomicOr(p.a.status, bad);
@@ -820,6 +864,11 @@ wk_status launch_paged_attention(wk_ctx* ctx, const PagedArgs& a, cudaStream_t s
   p.page16 = static_cast<uint32_t>(a.c.page_stride * es / 16);
   p.token16 = static_cast<uint32_t>(a.c.token_stride * es / 16);
   p.head_bytes = a.c.head_stride * es;
+  // with l the least power for which 2^l >= page: 2^(31 + l) / page, rounded up, errs by less than 2^l / 2^(31 + l) per position
+  uint32_t l = 0;
+  while ((1ull << l) < static_cast<uint64_t>(a.c.page_tokens)) ++l;
+  p.page_shift = 31 + l;
+  p.page_mul = static_cast<uint32_t>(((1ull << (31 + l)) + a.c.page_tokens - 1) / a.c.page_tokens);
   p.counter_bytes = static_cast<int32_t>(counter_bytes(ctx->sm_count));
   if (a.c.type == WK_BF16) return choose<WK_BF16, true>(ctx, p, nt, s);
   if (a.c.type == WK_F16) return choose<WK_F16, false>(ctx, p, nt, s);
