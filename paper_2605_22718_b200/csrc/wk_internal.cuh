@@ -205,7 +205,7 @@ wk_status launch_retrieve_query(wk_ctx* ctx, int layer, const __nv_bfloat16* Q, 
                                 float* score_out, cudaStream_t s);
 
 // Token-level cache in pages (entry points in wk_paged_api.cu).
-constexpr int kPlanMaxReq = 4096;
+constexpr int kPlanMaxReq = 4096;   // four for each of 1,024 threads
 struct PlanArgs {
   int32_t n_pages, page_tokens, n_req;
   const int32_t *lens, *more;
