@@ -120,6 +120,11 @@ __device__ __forceinline__ float hi_of(uint32_t w, bool bf16) {
   return bf16 ? __uint_as_float(w & 0xffff0000u) : __half2float(__ushort_as_half(static_cast<uint16_t>(w >> 16)));
 }
 using ptx::ex2_approx;
+__device__ __forceinline__ float warp_max(float x) {   // NaN counts for nothing
+  float y;
+  asm volatile("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(y) : "f"(x));
+  return y;
+}
 
 // ---------------------------------------------------------------- units
 // The line: for every unit of a request (kv heads first) the steps of all requests, one after the other.
@@ -129,10 +134,9 @@ struct Unit {
   int32_t shown, shift; // visible tokens; visible token j is position j, or j + shift from the sink's end on
 };
 
-// Steps that request r's units have each; 0: no request.
+// Steps that the units of a request of that length have each; 0: no request.
 template <int ST>
-__device__ __forceinline__ int32_t measure(const Params& p, int r, int32_t* shown, int32_t* shift) {
-  int32_t len = p.a.lens[r];
+__device__ __forceinline__ int32_t measure(const Params& p, int32_t len, int32_t* shown, int32_t* shift) {
   if (len < 0) return 0;
   len = min(len, p.room);
   *shown = p.a.window ? min(len, p.a.window + p.a.sink) : len;
@@ -158,28 +162,29 @@ __device__ __forceinline__ Unit locate(const Params& p, const uint32_t* pre, int
   uint32_t before = pre[lo];
   v.r = lo * per;
   v.shown = v.shift = 0;
-  v.cost = measure<ST>(p, v.r, &v.shown, &v.shift);
+  v.cost = measure<ST>(p, p.a.lens[v.r], &v.shown, &v.shift);
 #pragma unroll 1
   while (before + v.cost <= z && v.r < p.a.n_req - 1) {   // (z is less than the sum of all: the second bound is for lengths that change meanwhile)
     before += v.cost;
-    v.cost = measure<ST>(p, ++v.r, &v.shown, &v.shift);
+    v.cost = measure<ST>(p, p.a.lens[++v.r], &v.shown, &v.shift);
   }
   v.cost = max(v.cost, 1);
   v.left = v.cost - static_cast<int32_t>(z - before);
   return v;
 }
 
-// The unit behind v on the line.
+__device__ __forceinline__ int32_t request_after(const Params& p, int32_t r) { return r + 1 == p.a.n_req ? 0 : r + 1; }
+
+// The unit behind v on the line.  `ahead` is the length of the request behind v's, loaded a unit early.
 template <int ST>
-__device__ __forceinline__ void next_unit(const Params& p, Unit& v) {
+__device__ __forceinline__ void next_unit(const Params& p, Unit& v, int32_t& ahead) {
   int32_t skipped = 0;
 #pragma unroll 1
   do {
-    if (++v.r == p.a.n_req) {
-      v.r = 0;
-      ++v.u;
-    }
-    v.cost = measure<ST>(p, v.r, &v.shown, &v.shift);
+    v.r = request_after(p, v.r);
+    v.u += v.r == 0;
+    v.cost = measure<ST>(p, ahead, &v.shown, &v.shift);
+    ahead = p.a.lens[request_after(p, v.r)];
   } while (v.cost == 0 && ++skipped < p.a.n_req);   // (some request has steps: the bound is for lengths that change meanwhile)
   v.left = v.cost = max(v.cost, 1);
 }
@@ -228,20 +233,6 @@ struct Lane<64> {
     reinterpret_cast<uint32_t*>(static_cast<uint16_t*>(O) + i)[lane] = pack2<BF16>(v.x, v.y);
   }
 };
-// The share of the whole that each lane's log-sum-exp (log2) stands for; lse becomes that of the whole.
-__device__ __forceinline__ float join_weight(float& lse) {
-  float m = lse;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-  if (m == -INFINITY) m = 0.f;
-  const float e = ex2_approx(lse - m);
-  float l = e;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
-  lse = l == 0.f ? -INFINITY : m + __log2f(l);
-  return l == 0.f ? 0.f : __fdividef(e, l);
-}
-
 // ---------------------------------------------------------------- the kernel
 // Shared memory: a ring of STAGES steps per warp (at a warp's end also its last piece), the warps' first pieces, the steps' masks
 // and exponents.
@@ -257,7 +248,8 @@ paged_attention(const __grid_constant__ Params p) {
   __shared__ float plse[2 * W][8 * NT];
   __shared__ Piece piece[2 * W], split[2];
   __shared__ uint32_t masks[W][STAGES][S::RL];
-  __shared__ int32_t first[2], count[2], n_groups, group_at[2 * W + 1];
+  __shared__ int32_t to_come[W][4][3];   // units that the walk ahead has entered: request, unit, steps
+  __shared__ int32_t first[2], count[2], n_groups, group_at[2 * W + 1], order[2 * W];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
   uint8_t* const ring = dyn + warp * (STAGES * kStepBytes);
   uint8_t* const firsts = dyn + W * (STAGES * kStepBytes);
@@ -275,8 +267,9 @@ paged_attention(const __grid_constant__ Params p) {
     const int r = tid * per + i;
     int32_t shown, shift;
     if (r >= p.a.n_req) break;
-    mine += measure<ST>(p, r, &shown, &shift);
-    if (blockIdx.x == 0 && p.a.lens[r] > p.room && p.a.status) atomicOr(p.a.status, WK_DEV_BAD_SLOT);
+    const int32_t len = p.a.lens[r];
+    mine += measure<ST>(p, len, &shown, &shift);
+    if (blockIdx.x == 0 && len > p.room && p.a.status) atomicOr(p.a.status, WK_DEV_BAD_SLOT);
   }
   uint32_t up = mine;
 #pragma unroll
@@ -310,12 +303,15 @@ paged_attention(const __grid_constant__ Params p) {
     float sc[NT][2];               // logit scale of query heads 2c, 2c + 1
     float ref[NT][2], refw[NT][2]; // references of the sum and (8 bits) of the weights
     float sum[NT][2], o[NT][MT][4];
-    Unit cur = locate<ST, THREADS>(p, pre, per, all, x), nxt = cur;   // of the step at hand, of the one to look up
-    Heads hc = heads_of<NT>(p, cur.u);
+    Unit nxt = locate<ST, THREADS>(p, pre, per, all, x);   // of the step to look up; it is STAGES + 1 ahead
+    int32_t ahead = p.a.lens[request_after(p, nxt.r)];
+    int32_t cur_r = nxt.r, cur_u = nxt.u, cost = nxt.cost, left = nxt.left;   // of the step at hand
+    Heads hc = heads_of<NT>(p, cur_u);
     int32_t kv_up = hc.kv, kv_ask = hc.kv;   // kv heads of the step to look up, of the one to ask for
-    int32_t j_up = (cur.cost - cur.left) * ST + (lane & (ST - 1));   // this lane's token of the step to look up
-    const int32_t* table = p.a.tables + cur.r * p.a.table_stride;
-    bool whole = cur.left == cur.cost;       // the unit at hand began in this run
+    int32_t j_up = (cost - left) * ST + (lane & (ST - 1));   // this lane's token of the step to look up
+    const int32_t* table = p.a.tables + nxt.r * p.a.table_stride;
+    int in = 0, out = 0;                     // places in to_come
+    bool whole = left == cost;               // the unit at hand began in this run
     bool fresh = true;
     // Where this lane's chunks go: token k * RPI + lane / LPR, swizzled so that eight rows' chunks lie in different banks.
     const uint32_t ring_at = ptx::smem_u32(ring), chunk_l = lane % S::LPR, hi = lane / S::LPR;
@@ -356,7 +352,9 @@ paged_attention(const __grid_constant__ Params p) {
         if (i > -STAGES - 1) {
           j_up += ST;
           if (--nxt.left == 0) {
-            next_unit<ST>(p, nxt);
+            next_unit<ST>(p, nxt, ahead);
+            if (lane < 3) to_come[warp][in][lane] = lane == 0 ? nxt.r : lane == 1 ? nxt.u : nxt.cost;
+            in = (in + 1) & 3;   // (at most STAGES + 1 of them are waiting)
             kv_up = heads_of<NT>(p, nxt.u).kv;
             j_up = lane & (ST - 1);
             table = p.a.tables + nxt.r * p.a.table_stride;
@@ -601,13 +599,16 @@ paged_attention(const __grid_constant__ Params p) {
 
       // ---- does the unit end here, or this warp's part of it?
       if (i < -1) continue;
-      const bool over = i >= 0 && --cur.left == 0, ends = over || i + 1 == steps;
+      const bool over = i >= 0 && --left == 0, ends = over || i + 1 == steps;
       if (!ends && i >= 0) continue;
-      const Unit was = cur;
+      const int32_t was_r = cur_r, was_u = cur_u, was_cost = cost, was_done = cost - left;
       const Heads hw = hc;
       if (over && i + 1 < steps) {
-        next_unit<ST>(p, cur);
-        hc = heads_of<NT>(p, cur.u);
+        cur_r = to_come[warp][out][0];
+        cur_u = to_come[warp][out][1];
+        cost = left = to_come[warp][out][2];
+        out = (out + 1) & 3;
+        hc = heads_of<NT>(p, cur_u);
       }
       float f[NT][2];
       if (ends) {
@@ -627,7 +628,7 @@ paged_attention(const __grid_constant__ Params p) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
           const bool on = nt * 8 + g < hc.n;
-          const uint16_t* q = static_cast<const uint16_t*>(p.a.Q) + cur.r * p.a.q_stride + static_cast<int64_t>(hc.first + (on ? nt * 8 + g : 0)) * D;
+          const uint16_t* q = static_cast<const uint16_t*>(p.a.Q) + cur_r * p.a.q_stride + static_cast<int64_t>(hc.first + (on ? nt * 8 + g : 0)) * D;
 #pragma unroll
           for (int m = 0; m < MT; ++m) {
             if (E4) {
@@ -647,7 +648,7 @@ paged_attention(const __grid_constant__ Params p) {
           // transposed in registers: lane (g, c) then has head g's dimensions 2c, 2c + 1 of every 8 (8 bits: 4c .. 4c + 3 of 16)
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
-            const int64_t head = static_cast<int64_t>(was.r) * p.a.n_heads + hw.first + nt * 8;
+            const int64_t head = static_cast<int64_t>(was_r) * p.a.n_heads + hw.first + nt * 8;
             uint16_t* const to = static_cast<uint16_t*>(p.a.O) + (head + g) * D;
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
@@ -683,7 +684,7 @@ paged_attention(const __grid_constant__ Params p) {
                   rows[q * PADDED + m * 16 + (E4 ? 2 * g + h : 8 * h + g)] = o[nt][m][2 * h + e] * f[nt][e];
               if (g == 0) plse[which][q] = sum[nt][e];
             }
-          if (lane == 0) piece[which] = Piece{was.r, was.u, was.cost, x + i + 1 - (was.cost - was.left)};
+          if (lane == 0) piece[which] = Piece{was_r, was_u, was_cost, x + i + 1 - was_done};
         }
         whole = true;
       }
@@ -697,15 +698,16 @@ paged_attention(const __grid_constant__ Params p) {
   if (warp == 0) {
     static_assert(2 * W <= 32, "a lane per piece");
     const bool there = lane < 2 * W && piece[lane].r >= 0;
-    const uint32_t below = __ballot_sync(0xffffffffu, there) & ((1u << lane) - 1);
+    const uint32_t all_there = __ballot_sync(0xffffffffu, there), below = all_there & ((1u << lane) - 1);
     const int prev = below ? 31 - __clz(below) : lane;
     const bool start = there && (prev == lane || piece[prev].r != piece[lane].r || piece[prev].u != piece[lane].u);
     const uint32_t starts = __ballot_sync(0xffffffffu, start);
     if (lane < 2) split[lane].r = -1;
     __syncwarp();
+    if (there) order[__popc(below)] = lane;
     if (start) {
       const Piece u = piece[lane];
-      group_at[__popc(starts & ((1u << lane) - 1))] = lane;
+      group_at[__popc(starts & ((1u << lane) - 1))] = __popc(below);
       if (u.start < a0 || u.start + u.cost > a1) {
         const int side = u.start < a0 ? 0 : 1;
         split[side] = u;
@@ -715,7 +717,7 @@ paged_attention(const __grid_constant__ Params p) {
     }
     if (lane == 0) {
       n_groups = __popc(starts);
-      group_at[__popc(starts)] = 2 * W;
+      group_at[__popc(starts)] = __popc(all_there);
     }
   }
   __syncthreads();
@@ -724,19 +726,23 @@ paged_attention(const __grid_constant__ Params p) {
 #pragma unroll 1
   for (int it = warp; it < n_groups * rows; it += W) {
     const int k = it / rows, q = it - k * rows;
-    const int i0 = group_at[k], i1 = group_at[k + 1];
-    const Piece u = piece[i0];
+    const int i0 = group_at[k], n = group_at[k + 1] - i0;
+    const Piece u = piece[order[i0]];
     const Heads h = heads_of<NT>(p, u.u);
     if (q >= h.n) continue;
-    const bool there = i0 + lane < i1 && piece[i0 + lane].r >= 0;   // (fewer than 32 pieces)
-    float l = there ? plse[i0 + lane][q] : -INFINITY;
-    const float e = join_weight(l);
+    const float lse = lane < n ? plse[order[i0 + lane]][q] : -INFINITY;
+    float m = warp_max(lse), l = 0.f;
+    if (m == -INFINITY) m = 0.f;
+    const float e = ex2_approx(lse - m);
     Vec v = {};
-#pragma unroll 1
-    for (uint32_t m = __ballot_sync(0xffffffffu, there); m; m &= m - 1) {
-      const int i = __ffs(m) - 1;
-      Lane<D>::add(v, __shfl_sync(0xffffffffu, e, i), reinterpret_cast<const Vec*>(piece_rows(i0 + i) + q * PADDED)[lane]);
+#pragma unroll 2
+    for (int i = 0; i < n; ++i) {
+      const float w = __shfl_sync(0xffffffffu, e, i);
+      l += w;
+      Lane<D>::add(v, w, reinterpret_cast<const Vec*>(piece_rows(order[i0 + i]) + q * PADDED)[lane]);
     }
+    Lane<D>::scale(v, l == 0.f ? 0.f : __fdividef(1.f, l));
+    l = l == 0.f ? -INFINITY : m + __log2f(l);
     if (u.start >= a0 && u.start + u.cost <= a1) {
       const int64_t at = static_cast<int64_t>(u.r) * p.a.n_heads + h.first + q;
       Lane<D>::template store<QBF>(p.a.O, at * D, lane, v);
@@ -757,72 +763,82 @@ paged_attention(const __grid_constant__ Params p) {
     if (n) {
       __threadfence();   // the barrier has ordered the CTA's pieces before this
       mine = atomicInc(reinterpret_cast<uint32_t*>(p.a.scratch) + first[tid], n) == n;
-      __threadfence();
+      if (mine) __threadfence();
     }
     if (!mine) count[tid] = 0;
   }
   __syncthreads();
-  Vec* const part = reinterpret_cast<Vec*>(dyn);   // [W][32]
-  float* const sums = reinterpret_cast<float*>(dyn + W * 32 * sizeof(Vec));   // [W][2]
+  Vec* const part = reinterpret_cast<Vec*>(dyn);                              // [W][32]
+  float* const sums = reinterpret_cast<float*>(dyn + W * 32 * sizeof(Vec));   // [W][2]: reference and sum of a part
+  const int n0 = count[0] ? heads_of<NT>(p, split[0].u).n : 0, tasks = n0 + (count[1] ? heads_of<NT>(p, split[1].u).n : 0);
+  int lg = 0;   // 2^lg warps share a row, taking the pieces in turn
+  while (tasks << (lg + 1) <= W && lg < 5) ++lg;
 #pragma unroll 1
-  for (int side = 0; side < 2; ++side) {
-    const int n = count[side];
-    if (n == 0) continue;
-    const Piece u = split[side];
-    const Heads h = heads_of<NT>(p, u.u);
-    // A row belongs to one warp, or to several that take the pieces in turn.  The unit's first CTA has it as its last unit, the others
-    // as their first.
-    const int sets = max(W / h.n, 1);
+  for (int t0 = 0; t0 < tasks; t0 += W >> lg) {
+    const int task = t0 + (warp >> lg), set = warp & ((1 << lg) - 1);
+    const int side = task >= n0;
+    const bool on = task < tasks;
+    const int n = on ? count[side] : 0, q = task - (side ? n0 : 0);
+    float top = -INFINITY, l = 0.f;   // of this warp's pieces
+    Vec v = {};
+    // the unit's first CTA has it as its last unit, the others as their first
+    const float* const from = partial + (2 * first[side] + 1) * static_cast<int64_t>(kPieceFloats) + q;
+    auto piece_at = [&](int i) { return from + (i ? 2 * i - 1 : 0) * static_cast<int64_t>(kPieceFloats); };
 #pragma unroll 1
-    for (int q0 = 0; q0 < h.n; q0 += W / sets) {
-      const int q = q0 + warp / sets, set = warp % sets;
-      const bool on = q < h.n && warp < W / sets * sets;
-      Vec v = {};
-      float top = -INFINITY, l = 0.f;   // of this warp's pieces
-      if (on) {
-        const float* at = partial + (2 * first[side] + 1) * static_cast<int64_t>(kPieceFloats);
-#pragma unroll 1
-        for (int i0 = set; i0 < n; i0 += 32 * sets) {   // 32 of the pieces at a time
-          const int mine = i0 + lane * sets;
-          const float lse = mine < n ? __ldcg(at + (mine ? 2 * mine - 1 : 0) * static_cast<int64_t>(kPieceFloats) + q) : -INFINITY;
-          float m = lse;
+    for (int i0 = set; i0 < n; i0 += 32 << lg) {   // 32 of the pieces at a time
+      const int mine = i0 + (lane << lg), some = min((n - i0 + (1 << lg) - 1) >> lg, 32);
+      const float lse = mine < n ? __ldcg(piece_at(mine)) : -INFINITY;
+      Vec b[4];
 #pragma unroll
-          for (int d = 1; d < 32; d <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
-          m = fmaxf(m, top);
-          const float keep = m == -INFINITY ? 1.f : ex2_approx(top - m), e = ex2_approx(lse - (m == -INFINITY ? 0.f : m));
-          top = m;
-          float s = e;
+      for (int k = 0; k < 4; ++k)
+        if (k < some) b[k] = __ldcg(reinterpret_cast<const Vec*>(piece_at(i0 + (k << lg)) - q + 8 * NT + q * D) + lane);
+      const float m = fmaxf(warp_max(lse), top), keep = m == -INFINITY ? 1.f : ex2_approx(top - m);
+      const float e = ex2_approx(lse - (m == -INFINITY ? 0.f : m));
+      top = m;
+      l *= keep;
+      Lane<D>::scale(v, keep);
+#pragma unroll 1
+      for (int k0 = 0; k0 < some; k0 += 4) {
 #pragma unroll
-          for (int d = 1; d < 32; d <<= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-          l = l * keep + s;
-          Lane<D>::scale(v, keep);
-          const int in = min((n - i0 + sets - 1) / sets, 32);
-#pragma unroll 4
-          for (int k = 0; k < in; ++k) {
-            const int i = i0 + k * sets;
-            Lane<D>::add(v, __shfl_sync(0xffffffffu, e, k),
-                         __ldcg(reinterpret_cast<const Vec*>(at + (i ? 2 * i - 1 : 0) * static_cast<int64_t>(kPieceFloats) + 8 * NT + q * D) + lane));
+        for (int k = 0; k < 4; ++k)
+          if (k0 + k < some) {
+            const float w = __shfl_sync(0xffffffffu, e, k0 + k);
+            l += w;
+            Lane<D>::add(v, w, b[k]);
           }
-        }
-        part[warp * 32 + lane] = v;
-        if (lane == 0) {
-          sums[2 * warp] = l == 0.f ? -INFINITY : top + __log2f(l);
-          sums[2 * warp + 1] = l == 0.f ? 0.f : __fdividef(1.f, l);
-        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          if (k0 + 4 + k < some) b[k] = __ldcg(reinterpret_cast<const Vec*>(piece_at(i0 + ((k0 + 4 + k) << lg)) - q + 8 * NT + q * D) + lane);
       }
-      __syncthreads();
-      if (on && set == 0) {
-        float lse = lane < sets ? sums[2 * (warp + lane)] : -INFINITY;
-        const float e = join_weight(lse) * (lane < sets ? sums[2 * (warp + lane) + 1] : 0.f);
-        Vec w = {};
-#pragma unroll 1
-        for (int k = 0; k < sets; ++k) Lane<D>::add(w, __shfl_sync(0xffffffffu, e, k), part[(warp + k) * 32 + lane]);
-        const int64_t to = static_cast<int64_t>(u.r) * p.a.n_heads + h.first + q;
-        Lane<D>::template store<QBF>(p.a.O, to * D, lane, w);
-        if (lane == 0 && p.a.lse) p.a.lse[to] = lse * kLn2;
-      }
-      __syncthreads();
     }
+    if (lg) {
+      part[warp * 32 + lane] = v;
+      if (lane == 0) {
+        sums[2 * warp] = top;
+        sums[2 * warp + 1] = l;
+      }
+      __syncthreads();
+      if (set == 0) {
+        const float t = lane < 1 << lg ? sums[2 * (warp + lane)] : -INFINITY, s = lane < 1 << lg ? sums[2 * (warp + lane) + 1] : 0.f;
+        top = warp_max(t);
+        const float e = ex2_approx(t - (top == -INFINITY ? 0.f : top));
+        l = 0.f;
+        v = {};
+#pragma unroll 1
+        for (int k = 0; k < 1 << lg; ++k) {
+          const float w = __shfl_sync(0xffffffffu, e, k);
+          l += w * __shfl_sync(0xffffffffu, s, k);
+          Lane<D>::add(v, w, part[(warp + k) * 32 + lane]);
+        }
+      }
+    }
+    if (on && set == 0) {
+      Lane<D>::scale(v, l == 0.f ? 0.f : __fdividef(1.f, l));
+      const int64_t to = static_cast<int64_t>(split[side].r) * p.a.n_heads + heads_of<NT>(p, split[side].u).first + q;
+      Lane<D>::template store<QBF>(p.a.O, to * D, lane, v);
+      if (lane == 0 && p.a.lse) p.a.lse[to] = l == 0.f ? -INFINITY : (top + __log2f(l)) * kLn2;
+    }
+    if (lg) __syncthreads();
   }
 }
 
