@@ -269,8 +269,8 @@ enum { WK_BF16 = 0, WK_F16 = 1, WK_E4M3 = 2 };
 typedef struct {
   void* K;               /* [n_pages][page_tokens][n_kv_heads][head_dim], places given by the strides; 16-byte aligned */
   void* V;               /* the same layout */
-  uint8_t* K_exp;        /* WK_E4M3: [n_pages][n_kv_heads][page_tokens], contiguous: a row stands for its codes times */
-  uint8_t* V_exp;        /*   2^(byte - 127), byte in 1 .. 254; otherwise NULL */
+  uint8_t* K_exp;        /* WK_E4M3: [n_pages][n_kv_heads][page_tokens], contiguous, 4-byte aligned: a row stands for its */
+  uint8_t* V_exp;        /*   codes times 2^(byte - 127), byte in 1 .. 254; otherwise NULL */
   int64_t page_stride;   /* elements, multiples of 16 bytes, the rows of a cache not overlapping */
   int64_t token_stride;
   int64_t head_stride;

@@ -13,6 +13,7 @@ static wk_status check_cache(const wk_paged_kv* c) {
   if (c->head_dim != 64 && c->head_dim != 128) return WK_ERR_ARG;
   if (c->n_pages < 1 || c->page_tokens < 1 || c->n_kv_heads < 1 || c->reserved != 0) return WK_ERR_ARG;
   if ((c->type == WK_E4M3) != (c->K_exp != nullptr) || (c->type == WK_E4M3) != (c->V_exp != nullptr)) return WK_ERR_ARG;
+  if ((reinterpret_cast<uintptr_t>(c->K_exp) & 3u) || (reinterpret_cast<uintptr_t>(c->V_exp) & 3u)) return WK_ERR_ARG;
   const int64_t unit = c->type == WK_E4M3 ? 16 : 8;   // elements in 16 bytes
   // From the innermost axis out, each stride steps over all of what the axis inside it covers: no two rows share a byte.
   struct { int64_t stride, n; } ax[3] = {{c->page_stride, c->n_pages}, {c->token_stride, c->page_tokens}, {c->head_stride, c->n_kv_heads}};

@@ -60,13 +60,16 @@ struct Shape {
   static constexpr int RPI = 32 / LPR;                   // rows per copy instruction
   static constexpr int PADDED = D + 4;
   static constexpr int PIECE = 8 * NT * PADDED * 4;      // bytes of a piece in shared memory
-  static constexpr int META = MODE == WK_E4M3 ? 2 * ST : 0;   // bytes of a step's exponents, K's and V's side by side
+  static constexpr int META = MODE == WK_E4M3 ? 8 * ST : 0;   // bytes of a step's exponents: the word with K's, the word with V's
 };
 
 // ---------------------------------------------------------------- instructions
 __device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint32_t skip) {   // zeros, and nothing read, where skip is not 0
   asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\tcp.async.cg.shared.global [%0], [%1], 16, p;\n\t}"
                ::"r"(dst), "l"(src), "r"(skip) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -247,7 +250,7 @@ paged_attention(const __grid_constant__ Params p) {
   __shared__ uint32_t pre[THREADS], parts[W];
   __shared__ float plse[2 * W][8 * NT];
   __shared__ Piece piece[2 * W], split[2];
-  __shared__ uint32_t masks[W][STAGES][S::RL];
+  __shared__ uint32_t masks[W][STAGES][E4 ? 3 * S::RL : S::RL];   // which tokens there are; (8 bits) which byte of a word is theirs
   __shared__ int32_t to_come[W][4][3];   // units that the walk ahead has entered: request, unit, steps
   __shared__ int32_t first[2], count[2], n_groups, group_at[2 * W + 1], order[2 * W];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
@@ -298,7 +301,7 @@ paged_attention(const __grid_constant__ Params p) {
     const int32_t steps = static_cast<int32_t>(min(run, a1 - x));
     uint32_t bad = 0;
     int32_t id[S::RL];             // page ids of the step after the next one to ask for, and places in the page
-    uint32_t off[S::RL], row[S::RL], kx[S::RL], vx[S::RL];
+    uint32_t off[S::RL], row[S::RL], ex[S::RL];   // ex: place of the row's exponent bytes
     uint32_t qf[NT][MT][2];
     float sc[NT][2];               // logit scale of query heads 2c, 2c + 1
     float ref[NT][2], refw[NT][2]; // references of the sum and (8 bits) of the weights
@@ -323,16 +326,6 @@ paged_attention(const __grid_constant__ Params p) {
     for (int32_t i = -STAGES - 1; i < steps; ++i) {
       // ---- step i + STAGES: its page ids have come; rows of its tokens, a token per lane (or two)
       const bool ask = i >= -STAGES && i + STAGES < steps;
-      if constexpr (E4) {   // the exponents of the step asked for last have come, too
-        if (i > -STAGES && i + STAGES <= steps) {
-          uint8_t* const to = exps + (slot ? slot - 1 : STAGES - 1) * S::META + 2 * (lane & (ST - 1));
-#pragma unroll
-          for (int k = 0; k < S::RL; ++k) {
-            to[64 * k] = static_cast<uint8_t>(kx[k]);
-            to[64 * k + 1] = static_cast<uint8_t>(vx[k]);
-          }
-        }
-      }
       if (ask) {
         kv_ask = kv_up;
 #pragma unroll
@@ -340,11 +333,8 @@ paged_attention(const __grid_constant__ Params p) {
           const bool there = static_cast<uint32_t>(id[k]) < static_cast<uint32_t>(p.a.c.n_pages);
           if (!there && id[k] != -1) bad = WK_DEV_BAD_SLOT;
           row[k] = there ? id[k] * p.page16 + off[k] * p.token16 : kNowhere;
-          if constexpr (E4) {
-            const int64_t e = there ? (static_cast<int64_t>(id[k]) * p.a.c.n_kv_heads + kv_ask) * p.a.c.page_tokens + off[k] : 0;
-            kx[k] = __ldg(p.a.c.K_exp + e);   // (of any token where there is none)
-            vx[k] = __ldg(p.a.c.V_exp + e);
-          }
+          // (fewer than 2^30 rows: there are 64 bytes to each, and less than 64 GB)
+          if constexpr (E4) ex[k] = there ? (id[k] * p.a.c.n_kv_heads + kv_ask) * p.a.c.page_tokens + off[k] : 0;
         }
       }
       // ---- step i + STAGES + 1: look up the page ids
@@ -462,12 +452,19 @@ paged_attention(const __grid_constant__ Params p) {
         float top[NT][2], topw[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) top[nt][0] = top[nt][1] = topw[nt][0] = topw[nt][1] = -INFINITY;
+        float vpower[E4 ? ST / 16 : 1][2];
 #pragma unroll
         for (int t = 0; t < ST / 16; ++t)
 #pragma unroll
           for (int hh = 0; hh < 2; ++hh) {
             float kscale = 1.f;
-            if constexpr (E4) kscale = __uint_as_float(static_cast<uint32_t>(exps[slot * S::META + 2 * (t * 16 + hh * 8 + g)]) << 23);
+            if constexpr (E4) {
+              const int at = t % 2 * 16 + hh * 8 + g;
+              const uint2 w2 = *reinterpret_cast<const uint2*>(exps + slot * S::META + 8 * (t * 16 + hh * 8 + g));
+              const uint32_t byte = (masks[warp][slot][S::RL + t / 2 * 2] >> at & 1) | (masks[warp][slot][S::RL + t / 2 * 2 + 1] >> at & 1) << 1;
+              kscale = __uint_as_float((w2.x >> (8 * byte) & 255u) << 23);
+              vpower[t][hh] = static_cast<float>(static_cast<int>(w2.y >> (8 * byte) & 255u) - 127);
+            }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -491,8 +488,6 @@ paged_attention(const __grid_constant__ Params p) {
         for (int t = 0; t < ST / 16; ++t)
 #pragma unroll
           for (int hh = 0; hh < 2; ++hh) {
-            float vpower = 0.f;
-            if constexpr (E4) vpower = static_cast<float>(static_cast<int>(exps[slot * S::META + 2 * (t * 16 + hh * 8 + g) + 1]) - 127);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -500,8 +495,8 @@ paged_attention(const __grid_constant__ Params p) {
                 const float v = s[t][nt][2 * hh + e];
                 top[nt][e] = fmaxf(top[nt][e], v);
                 if constexpr (E4) {
-                  w[t][nt][2 * hh + e] = v + vpower;
-                  topw[nt][e] = fmaxf(topw[nt][e], v + vpower);
+                  w[t][nt][2 * hh + e] = v + vpower[t][hh];
+                  topw[nt][e] = fmaxf(topw[nt][e], v + vpower[t][hh]);
                 }
               }
           }
@@ -592,6 +587,16 @@ paged_attention(const __grid_constant__ Params p) {
         for (int k = 0; k < S::RL; ++k) {
           const uint32_t mask = __ballot_sync(0xffffffffu, row[k] != kNowhere);
           if (lane == 0) masks[warp][slot][k] = mask;
+          if constexpr (E4) {   // aligned words are what can be copied asynchronously: they hold the byte, and lie in the array's memory
+            const uint32_t to_ex = ptx::smem_u32(exps) + slot * S::META + 8 * ((lane & (ST - 1)) + 32 * k);
+            copy4(to_ex, p.a.c.K_exp + (ex[k] & ~3u));
+            copy4(to_ex + 4, p.a.c.V_exp + (ex[k] & ~3u));
+            const uint32_t lo = __ballot_sync(0xffffffffu, ex[k] & 1), hi2 = __ballot_sync(0xffffffffu, ex[k] & 2);
+            if (lane == 0) {
+              masks[warp][slot][S::RL + 2 * k] = lo;
+              masks[warp][slot][S::RL + 2 * k + 1] = hi2;
+            }
+          }
         }
       }
       copies_commit();
@@ -735,7 +740,7 @@ paged_attention(const __grid_constant__ Params p) {
     if (m == -INFINITY) m = 0.f;
     const float e = ex2_approx(lse - m);
     Vec v = {};
-#pragma unroll 2
+#pragma unroll 4
     for (int i = 0; i < n; ++i) {
       const float w = __shfl_sync(0xffffffffu, e, i);
       l += w;

@@ -58,7 +58,7 @@ E4M3 = dict(type=binding.WK_E4M3, K_exp=P, V_exp=P)
 BAD_CACHES = [
     (dict(K=None), ARG), (dict(V=None), ARG), (dict(K=P + 8), ARG), (dict(V=P + 2), ARG), (dict(type=3), ARG), (dict(type=-1), ARG),
     (dict(head_dim=96), ARG), (dict(head_dim=0), ARG), (dict(n_pages=0), ARG), (dict(page_tokens=0), ARG), (dict(n_kv_heads=0), ARG),
-    (dict(reserved=1), ARG), (dict(K_exp=P), ARG), (dict(type=binding.WK_E4M3), ARG), (dict(E4M3, V_exp=None), ARG),
+    (dict(reserved=1), ARG), (dict(K_exp=P), ARG), (dict(type=binding.WK_E4M3), ARG), (dict(E4M3, V_exp=None), ARG), (dict(E4M3, K_exp=P + 2), ARG), (dict(E4M3, V_exp=P + 1), ARG),
     (dict(token_stride=8 * 128 + 4), ARG), (dict(head_stride=127), ARG), (dict(page_stride=-16 * 8 * 128), ARG),
     (dict(E4M3, token_stride=8 * 128 + 8), ARG),                       # 8 bytes
     (dict(head_stride=120), ARG), (dict(token_stride=7 * 128), ARG), (dict(page_stride=15 * 8 * 128), ARG),   # rows overlap
