@@ -5,9 +5,10 @@
 // flight.
 //
 //   * Work.  A unit is (request, kv head, up to 8 * NT of the query heads that share it).  A unit's tokens are cut into steps of ST
-//     tokens (8 KB of K and V); all steps of all units form one line, and every CTA takes an equal run of it (one CTA per SM),
-//     every warp an equal run of the CTA's.  So lengths of any spread load all SMs alike, the grid does not depend on the lengths
-//     (a captured call follows them), and a unit is cut only where a run ends.  The lengths are summed by every CTA for itself.
+//     tokens (8 KB of K and V); all steps of all units form one line (or several of the same length), and every CTA takes an equal
+//     run of it (one CTA per SM), every warp an equal run of the CTA's.  So lengths of any spread load all SMs alike, the grid does
+//     not depend on the lengths (a captured call follows them), and a unit is cut only where a run ends.  The lengths are summed by
+//     every CTA for itself.
 //   * A warp walks its run alone, without barriers: it copies the rows of coming steps into its own ring in shared memory
 //     (16-byte asynchronous copies, tokens that are not attended become zeros) and multiplies out of it.  Page ids are looked up
 //     a step before their rows are asked for.
@@ -35,10 +36,12 @@ constexpr uint32_t kNowhere = 0xffffffffu;   // row offset of a token that is no
 constexpr float kLazy = 8.f;                 // how far (log2) a logit may exceed the reference
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 constexpr int kStepBytes = 8192;             // of K and V in a step
+constexpr int kLongRun = 24;                 // steps per warp from which on heads are walked side by side
 
 struct Params {
   PagedArgs a;
   int32_t group, q_tiles, units;   // query heads per kv head, units of a kv head, units of a request
+  int32_t lines;                   // lines that CTAs walk side by side (where runs are long): a divisor of `units`
   int32_t room;                    // positions that a table can name
   uint32_t page16, token16;        // strides in units of 16 bytes
   int64_t head_bytes;              // stride of a kv head
@@ -130,7 +133,8 @@ __device__ __forceinline__ float warp_max(float x) {   // NaN counts for nothing
 }
 
 // ---------------------------------------------------------------- units
-// The line: for every unit of a request (kv heads first) the steps of all requests, one after the other.
+// A line: for one unit of a request (kv heads first) the steps of all requests, one after the other, then the same for another unit.
+// Units are dealt to the lines in turn: line i of n has units i, i + n, ...
 struct Unit {
   int32_t r, u;         // request, unit of the request
   int32_t cost, left;   // steps of the unit (at least one, also where nothing is visible), those from the one at hand on
@@ -153,7 +157,8 @@ __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
   return (a | b) >> 32 ? quotient64(a, b) : static_cast<int64_t>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b));
 }
 
-// The unit that place x of the line lies in.  pre[t]: steps of the requests before thread t's `per` requests, of all: `all`.
+// The unit that place x of a line lies in (u: counted in the line).  pre[t]: steps of the requests before thread t's `per`
+// requests, of all: `all`.
 template <int ST, int THREADS>
 __device__ __forceinline__ Unit locate(const Params& p, const uint32_t* pre, int per, uint32_t all, int64_t x) {
   Unit v;
@@ -180,12 +185,12 @@ __device__ __forceinline__ int32_t request_after(const Params& p, int32_t r) { r
 
 // The unit behind v on the line.  `ahead` is the length of the request behind v's, loaded a unit early.
 template <int ST>
-__device__ __forceinline__ void next_unit(const Params& p, Unit& v, int32_t& ahead) {
+__device__ __forceinline__ void next_unit(const Params& p, Unit& v, int32_t& ahead, int32_t lines) {
   int32_t skipped = 0;
 #pragma unroll 1
   do {
     v.r = request_after(p, v.r);
-    v.u += v.r == 0;
+    if (v.r == 0) v.u += lines;
     v.cost = measure<ST>(p, ahead, &v.shown, &v.shift);
     ahead = p.a.lens[request_after(p, v.r)];
   } while (v.cost == 0 && ++skipped < p.a.n_req);   // (some request has steps: the bound is for lengths that change meanwhile)
@@ -290,10 +295,14 @@ paged_attention(const __grid_constant__ Params p) {
   }
   pre[tid] = before + up - mine;
   __syncthreads();
-  const int64_t total = static_cast<int64_t>(all) * p.units;
-  const int64_t run = quotient(total + gridDim.x * W - 1, gridDim.x * W), chunk = run * W;
-  const int64_t a0 = blockIdx.x * chunk, a1 = min(a0 + chunk, total);
-  if (a0 >= total) return;
+  // CTA k * lines + line takes the k-th run of a line; for short runs side by side is not worth the SMs that are left over.
+  const int lines = p.lines > 1 && static_cast<int64_t>(all) * p.units >= kLongRun * static_cast<int64_t>(gridDim.x * W) ? p.lines : 1;
+  const int line = lines == 1 ? 0 : blockIdx.x % lines, column = lines == 1 ? blockIdx.x : blockIdx.x / lines;
+  const int64_t length = static_cast<int64_t>(all) * (lines == 1 ? p.units : p.units / lines), line0 = line * length;
+  const uint32_t workers = (lines == 1 ? gridDim.x : gridDim.x / lines) * W;
+  const int64_t run = quotient(length + workers - 1, workers), chunk = run * W;
+  const int64_t a0 = line0 + column * chunk, a1 = min(a0 + chunk, line0 + length);
+  if (a0 >= a1) return;
   const int64_t x = a0 + warp * run;
   if (lane < 2) piece[2 * warp + lane].r = -1;
 
@@ -306,7 +315,8 @@ paged_attention(const __grid_constant__ Params p) {
     float sc[NT][2];               // logit scale of query heads 2c, 2c + 1
     float ref[NT][2], refw[NT][2]; // references of the sum and (8 bits) of the weights
     float sum[NT][2], o[NT][MT][4];
-    Unit nxt = locate<ST, THREADS>(p, pre, per, all, x);   // of the step to look up; it is STAGES + 1 ahead
+    Unit nxt = locate<ST, THREADS>(p, pre, per, all, x - line0);   // of the step to look up; it is STAGES + 1 ahead
+    nxt.u = nxt.u * lines + line;
     int32_t ahead = p.a.lens[request_after(p, nxt.r)];
     int32_t cur_r = nxt.r, cur_u = nxt.u, cost = nxt.cost, left = nxt.left;   // of the step at hand
     Heads hc = heads_of<NT>(p, cur_u);
@@ -342,7 +352,7 @@ paged_attention(const __grid_constant__ Params p) {
         if (i > -STAGES - 1) {
           j_up += ST;
           if (--nxt.left == 0) {
-            next_unit<ST>(p, nxt, ahead);
+            next_unit<ST>(p, nxt, ahead, lines);
             if (lane < 3) to_come[warp][in][lane] = lane == 0 ? nxt.r : lane == 1 ? nxt.u : nxt.cost;
             in = (in + 1) & 3;   // (at most STAGES + 1 of them are waiting)
             kv_up = heads_of<NT>(p, nxt.u).kv;
@@ -716,8 +726,9 @@ paged_attention(const __grid_constant__ Params p) {
       if (u.start < a0 || u.start + u.cost > a1) {
         const int side = u.start < a0 ? 0 : 1;
         split[side] = u;
-        first[side] = static_cast<int>(quotient(u.start, chunk));
-        count[side] = static_cast<int>(quotient(u.start + u.cost - 1, chunk)) - first[side] + 1;
+        const int k = static_cast<int>(quotient(u.start - line0, chunk));
+        first[side] = k * lines + line;   // the CTA that the unit begins in
+        count[side] = static_cast<int>(quotient(u.start + u.cost - 1 - line0, chunk)) - k + 1;
       }
     }
     if (lane == 0) {
@@ -776,8 +787,8 @@ paged_attention(const __grid_constant__ Params p) {
   Vec* const part = reinterpret_cast<Vec*>(dyn);                              // [W][32]
   float* const sums = reinterpret_cast<float*>(dyn + W * 32 * sizeof(Vec));   // [W][2]: reference and sum of a part
   const int n0 = count[0] ? heads_of<NT>(p, split[0].u).n : 0, tasks = n0 + (count[1] ? heads_of<NT>(p, split[1].u).n : 0);
-  int lg = 0;   // 2^lg warps share a row, taking the pieces in turn
-  while (tasks << (lg + 1) <= W && lg < 5) ++lg;
+  int lg = 0;   // 2^lg warps share a row, taking the pieces in turn (as many whoever arrives last: the order of the sums is fixed)
+  while (rows << (lg + 2) <= W) ++lg;
 #pragma unroll 1
   for (int t0 = 0; t0 < tasks; t0 += W >> lg) {
     const int task = t0 + (warp >> lg), set = warp & ((1 << lg) - 1);
@@ -788,7 +799,7 @@ paged_attention(const __grid_constant__ Params p) {
     Vec v = {};
     // the unit's first CTA has it as its last unit, the others as their first
     const float* const from = partial + (2 * first[side] + 1) * static_cast<int64_t>(kPieceFloats) + q;
-    auto piece_at = [&](int i) { return from + (i ? 2 * i - 1 : 0) * static_cast<int64_t>(kPieceFloats); };
+    auto piece_at = [&](int i) { return from + (2 * i * lines - (i != 0)) * static_cast<int64_t>(kPieceFloats); };
 #pragma unroll 1
     for (int i0 = set; i0 < n; i0 += 32 << lg) {   // 32 of the pieces at a time
       const int mine = i0 + (lane << lg), some = min((n - i0 + (1 << lg) - 1) >> lg, 32);
@@ -880,8 +891,16 @@ wk_status launch_paged_attention(wk_ctx* ctx, const PagedArgs& a, cudaStream_t s
   const int nt = p.group > 8 ? 2 : 1;
   p.q_tiles = (p.group + 8 * nt - 1) / (8 * nt);
   p.units = a.c.n_kv_heads * p.q_tiles;
-  p.room = a.max_pages * a.c.page_tokens;
   const int es = a.c.type == WK_E4M3 ? 1 : 2;
+  // Units of long requests are walked side by side, so that rows of neighbouring heads, neighbours in memory as a rule, are read at
+  // about the same time, and the rows of a kv head with more than 16 query heads once.  Rows of 128 bytes (8 bits), 16 x 20,000
+  // tokens of 8 heads: 121 us -> 107, of 16 heads 124 -> 107; of 64 bytes 112 -> 69; rows of 256 bytes gain nothing (197 -> 196).
+  // As many lines as leave hardly any SM over.
+  p.lines = 1;
+  if (a.c.head_dim * es < 256 || p.q_tiles > 1)
+    for (int d = 2; d <= 16; ++d)
+      if (p.units % d == 0 && ctx->sm_count / d * d >= ctx->sm_count - ctx->sm_count / 32) p.lines = d;
+  p.room = a.max_pages * a.c.page_tokens;
   p.page16 = static_cast<uint32_t>(a.c.page_stride * es / 16);
   p.token16 = static_cast<uint32_t>(a.c.token_stride * es / 16);
   p.head_bytes = a.c.head_stride * es;
