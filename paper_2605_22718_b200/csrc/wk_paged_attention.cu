@@ -267,6 +267,10 @@ paged_attention(const __grid_constant__ Params p) {
     return reinterpret_cast<float*>(i & 1 ? dyn + (i >> 1) * (STAGES * kStepBytes) : firsts + (i >> 1) * S::PIECE);
   };
 
+  // (launched while the kernel before it drains, and the one behind it likewise: nothing is read or written before this)
+  dep_release();
+  dep_wait();
+
   // ---- the line of steps, and this warp's run of it
   const int per = (p.a.n_req + THREADS - 1) / THREADS;
   uint32_t mine = 0;
@@ -867,7 +871,7 @@ wk_status launch(wk_ctx* ctx, const Params& p, cudaStream_t s) {
     WK_CUDA_TRY(ctx, cudaFuncSetAttribute(paged_attention<MODE, D, NT, QBF>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
     ctx->paged_attr_set |= 1u << i;
   }
-  paged_attention<MODE, D, NT, QBF><<<ctx->sm_count, 32 * S::W, smem, s>>>(p);
+  launch_chained(paged_attention<MODE, D, NT, QBF>, dim3(ctx->sm_count), dim3(32 * S::W), smem, s, p);
   return after_launch(ctx);
 }
 

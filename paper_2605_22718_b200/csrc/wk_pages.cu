@@ -62,6 +62,8 @@ page_plan(const __grid_constant__ PlanArgs a) {
   __shared__ uint32_t popped, found_by[kWarps];
   __shared__ int32_t last;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  dep_release();
+  dep_wait();   // nothing is read or written before the kernel in front has ended
   const int B = a.n_req, page = a.page_tokens;
   int32_t head = a.state[0], count = a.state[1];
   uint32_t bad = 0;
@@ -297,6 +299,8 @@ __device__ __forceinline__ bool slot_place(const StoreArgs& a, int32_t slot, int
 // first store.  head_dim is 64 or 128, so a head is 8 or 16 vectors.
 __global__ void __launch_bounds__(kStoreThreads)
 store_rows(const __grid_constant__ StoreArgs a) {
+  dep_release();
+  dep_wait();
   const int side = blockIdx.y;
   const int head_shift = a.c.head_dim == 128 ? 4 : 3;
   const int vecs = a.c.n_kv_heads << head_shift;
@@ -348,6 +352,8 @@ __global__ void __launch_bounds__(kStoreThreads)
 store_rows_e4m3(const __grid_constant__ StoreArgs a) {
   constexpr int LANES = D / 8, ROWS = kStoreThreads / LANES;   // lanes per row, rows at a time
   constexpr uint32_t kInf = BF16 ? 0x7f80u : 0x7c00u;
+  dep_release();
+  dep_wait();
   const int side = blockIdx.y, l = threadIdx.x % LANES;
   uint8_t* dst = static_cast<uint8_t*>(side ? a.c.V : a.c.K);
   uint8_t* exps = side ? a.c.V_exp : a.c.K_exp;
@@ -431,8 +437,8 @@ wk_status launch_page_plan(wk_ctx* ctx, const PlanArgs& a, cudaStream_t s) {
     const int64_t n = (static_cast<int64_t>(a.max_tokens) + 4 * threads - 1) / (4 * threads);
     return static_cast<int>(n < 1 ? 1 : n < ctx->sm_count ? n : ctx->sm_count);
   };
-  if (a.n_req <= kPlanPer * 256) page_plan<256><<<blocks(256), 256, 0, s>>>(a);
-  else page_plan<1024><<<blocks(1024), 1024, 0, s>>>(a);
+  if (a.n_req <= kPlanPer * 256) launch_chained(page_plan<256>, dim3(blocks(256)), dim3(256), 0, s, a);
+  else launch_chained(page_plan<1024>, dim3(blocks(1024)), dim3(1024), 0, s, a);
   return after_launch(ctx);
 }
 
@@ -453,9 +459,10 @@ wk_status launch_page_store(wk_ctx* ctx, const wk_paged_kv& c, const void* K_new
   a.rows = rows > 1 ? static_cast<int>(rows) : 1;
   const dim3 grid(static_cast<unsigned>((n_tokens + a.rows - 1) / a.rows), 2);
   const bool wide = c.head_dim == 128;
-  if (c.type != WK_E4M3) store_rows<<<grid, kStoreThreads, 0, s>>>(a);
-  else if (src_type == WK_BF16) wide ? store_rows_e4m3<true, 128><<<grid, kStoreThreads, 0, s>>>(a) : store_rows_e4m3<true, 64><<<grid, kStoreThreads, 0, s>>>(a);
-  else wide ? store_rows_e4m3<false, 128><<<grid, kStoreThreads, 0, s>>>(a) : store_rows_e4m3<false, 64><<<grid, kStoreThreads, 0, s>>>(a);
+  void (*kernel)(const StoreArgs) = store_rows;
+  if (c.type == WK_E4M3 && src_type == WK_BF16) kernel = wide ? store_rows_e4m3<true, 128> : store_rows_e4m3<true, 64>;
+  else if (c.type == WK_E4M3) kernel = wide ? store_rows_e4m3<false, 128> : store_rows_e4m3<false, 64>;
+  launch_chained(kernel, grid, dim3(kStoreThreads), 0, s, a);
   return after_launch(ctx);
 }
 
