@@ -36,6 +36,7 @@ constexpr uint32_t kNowhere = 0xffffffffu;   // row offset of a token that is no
 constexpr float kLazy = 8.f;                 // how far (log2) a logit may exceed the reference
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 constexpr int kStepBytes = 8192;             // of K and V in a step
+constexpr int kShortRun = 4, kWhole = 8;     // where runs are that short, CTAs go round units of up to so many steps
 constexpr int kLongRun = 24;                 // steps per warp from which on heads are walked side by side
 
 struct Params {
@@ -134,10 +135,11 @@ __device__ __forceinline__ float warp_max(float x) {   // NaN counts for nothing
 
 // ---------------------------------------------------------------- units
 // A line: for one unit of a request (kv heads first) the steps of all requests, one after the other, then the same for another unit.
-// Units are dealt to the lines in turn: line i of n has units i, i + n, ...
+// Units are dealt to the lines in turn: line i of n has units i, i + n, ...  A place of the line before every unit's first step stands
+// for what a unit costs by itself (about a step's time).
 struct Unit {
   int32_t r, u;         // request, unit of the request
-  int32_t cost, left;   // steps of the unit (at least one, also where nothing is visible), those from the one at hand on
+  int32_t steps, left;  // of the unit (at least one, also where nothing is visible), those from the one at hand on
   int32_t shown, shift; // visible tokens; visible token j is position j, or j + shift from the sink's end on
 };
 
@@ -157,10 +159,29 @@ __device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
   return (a | b) >> 32 ? quotient64(a, b) : static_cast<int64_t>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b));
 }
 
-// The unit that place x of a line lies in (u: counted in the line).  pre[t]: steps of the requests before thread t's `per`
-// requests, of all: `all`.
+__device__ __forceinline__ uint32_t places(int32_t steps) { return steps ? steps + 1u : 0u; }
+
+__device__ __forceinline__ int32_t request_after(const Params& p, int32_t r) { return r + 1 == p.a.n_req ? 0 : r + 1; }
+
+// The unit behind v on its line.  `ahead` is the length of the request behind v's, loaded a unit early.
+template <int ST>
+__device__ __forceinline__ void next_unit(const Params& p, Unit& v, int32_t& ahead, int32_t lines) {
+  int32_t skipped = 0;
+#pragma unroll 1
+  do {
+    v.r = request_after(p, v.r);
+    if (v.r == 0) v.u += lines;
+    v.steps = measure<ST>(p, ahead, &v.shown, &v.shift);
+    ahead = p.a.lens[request_after(p, v.r)];
+  } while (v.steps == 0 && ++skipped < p.a.n_req);   // (some request has steps: the bound is for lengths that change meanwhile)
+  v.left = v.steps = max(v.steps, 1);
+}
+
+// What a run that begins at place x of a line begins with: the step at x or the first one behind it; with `uncut`, inside a unit of few
+// steps, the unit's first step or the next unit's, whichever is nearer (only the place is told then).
+// *at: that step's place.  u: counted in the line.  pre[t]: places of the requests before thread t's `per` requests, of all: `all`.
 template <int ST, int THREADS>
-__device__ __forceinline__ Unit locate(const Params& p, const uint32_t* pre, int per, uint32_t all, int64_t x) {
+__device__ __forceinline__ Unit locate(const Params& p, const uint32_t* pre, int per, uint32_t all, int64_t x, bool uncut, int64_t* at) {
   Unit v;
   v.u = static_cast<int32_t>(quotient(x, all));
   const uint32_t z = static_cast<uint32_t>(x - static_cast<int64_t>(v.u) * all);
@@ -170,31 +191,18 @@ __device__ __forceinline__ Unit locate(const Params& p, const uint32_t* pre, int
   uint32_t before = pre[lo];
   v.r = lo * per;
   v.shown = v.shift = 0;
-  v.cost = measure<ST>(p, p.a.lens[v.r], &v.shown, &v.shift);
+  v.steps = measure<ST>(p, p.a.lens[v.r], &v.shown, &v.shift);
 #pragma unroll 1
-  while (before + v.cost <= z && v.r < p.a.n_req - 1) {   // (z is less than the sum of all: the second bound is for lengths that change meanwhile)
-    before += v.cost;
-    v.cost = measure<ST>(p, p.a.lens[++v.r], &v.shown, &v.shift);
+  while (before + places(v.steps) <= z && v.r < p.a.n_req - 1) {   // (z is less than the sum of all: the second bound is for lengths that change meanwhile)
+    before += places(v.steps);
+    v.steps = measure<ST>(p, p.a.lens[++v.r], &v.shown, &v.shift);
   }
-  v.cost = max(v.cost, 1);
-  v.left = v.cost - static_cast<int32_t>(z - before);
+  v.steps = max(v.steps, 1);
+  int32_t step = max(static_cast<int32_t>(z - before) - 1, 0);
+  if (uncut && v.steps <= kWhole) step = 2 * (z - before) >= places(v.steps) ? v.steps + 1 : 0;
+  *at = static_cast<int64_t>(v.u) * all + before + 1 + step;
+  v.left = v.steps - step;
   return v;
-}
-
-__device__ __forceinline__ int32_t request_after(const Params& p, int32_t r) { return r + 1 == p.a.n_req ? 0 : r + 1; }
-
-// The unit behind v on the line.  `ahead` is the length of the request behind v's, loaded a unit early.
-template <int ST>
-__device__ __forceinline__ void next_unit(const Params& p, Unit& v, int32_t& ahead, int32_t lines) {
-  int32_t skipped = 0;
-#pragma unroll 1
-  do {
-    v.r = request_after(p, v.r);
-    if (v.r == 0) v.u += lines;
-    v.cost = measure<ST>(p, ahead, &v.shown, &v.shift);
-    ahead = p.a.lens[request_after(p, v.r)];
-  } while (v.cost == 0 && ++skipped < p.a.n_req);   // (some request has steps: the bound is for lengths that change meanwhile)
-  v.left = v.cost = max(v.cost, 1);
 }
 
 struct Heads {
@@ -212,8 +220,8 @@ __device__ __forceinline__ Heads heads_of(const Params& p, int u) {
 
 // What the warps and CTAs that share a unit leave each other.
 struct Piece {
-  int32_t r, u, cost;   // r < 0: none
-  int64_t start;        // the unit's first place in the line
+  int32_t r, u, steps;  // r < 0: none
+  int64_t start;        // place of the unit's first step
 };
 constexpr int kPieceFloats = 16 * (128 + 1);   // of a piece in the scratch buffer: log-sum-exps, then rows
 constexpr size_t counter_bytes(int ctas) { return (ctas * sizeof(uint32_t) + 255) / 256 * 256; }
@@ -280,7 +288,7 @@ paged_attention(const __grid_constant__ Params p) {
     int32_t shown, shift;
     if (r >= p.a.n_req) break;
     const int32_t len = p.a.lens[r];
-    mine += measure<ST>(p, len, &shown, &shift);
+    mine += places(measure<ST>(p, len, &shown, &shift));
     if (blockIdx.x == 0 && len > p.room && p.a.status) atomicOr(p.a.status, WK_DEV_BAD_SLOT);
   }
   uint32_t up = mine;
@@ -304,14 +312,25 @@ paged_attention(const __grid_constant__ Params p) {
   const int line = lines == 1 ? 0 : blockIdx.x % lines, column = lines == 1 ? blockIdx.x : blockIdx.x / lines;
   const int64_t length = static_cast<int64_t>(all) * (lines == 1 ? p.units : p.units / lines), line0 = line * length;
   const uint32_t workers = (lines == 1 ? gridDim.x : gridDim.x / lines) * W;
-  const int64_t run = quotient(length + workers - 1, workers), chunk = run * W;
-  const int64_t a0 = line0 + column * chunk, a1 = min(a0 + chunk, line0 + length);
-  if (a0 >= a1) return;
-  const int64_t x = a0 + warp * run;
+  int64_t run = quotient(length + workers - 1, workers);
+  const int64_t chunk = run * W;
+  if (column * chunk >= length) return;
   if (lane < 2) piece[2 * warp + lane].r = -1;
+  // Short runs of short units: a CTA's run begins and ends with a unit, for a join of CTAs costs more than a few steps (20 requests of 55 tokens,
+  // 8 heads of 64: 8.7 us -> 7.0; where runs are longer, cuts anywhere balance them: 256 requests of up to 300 tokens, 16 heads of 64, 21.2 us,
+  // 23.2 if they went round units).
+  int64_t a0 = column * chunk, a1 = min(a0 + chunk, length);
+  if (run <= kShortRun && all <= 2u * kWhole * p.a.n_req) {
+    const int64_t from = a0, to = a1;
+    if (from > 0) locate<ST, THREADS>(p, pre, per, all, from, true, &a0);
+    if (to < length) locate<ST, THREADS>(p, pre, per, all, to, true, &a1);
+    run = max(a1 - a0 + W - 1, static_cast<int64_t>(0)) / W;
+  }
+  const int64_t x = a0 + warp * run, xe = min(x + run, a1);
+  a0 += line0;
+  a1 += line0;
 
-  if (x < a1) {
-    const int32_t steps = static_cast<int32_t>(min(run, a1 - x));
+  if (x < xe) {
     uint32_t bad = 0;
     int32_t id[S::RL];             // page ids of the step after the next one to ask for, and places in the page
     uint32_t off[S::RL], row[S::RL], ex[S::RL];   // ex: place of the row's exponent bytes
@@ -319,16 +338,20 @@ paged_attention(const __grid_constant__ Params p) {
     float sc[NT][2];               // logit scale of query heads 2c, 2c + 1
     float ref[NT][2], refw[NT][2]; // references of the sum and (8 bits) of the weights
     float sum[NT][2], o[NT][MT][4];
-    Unit nxt = locate<ST, THREADS>(p, pre, per, all, x - line0);   // of the step to look up; it is STAGES + 1 ahead
+    int64_t place;                 // of the step at hand
+    Unit nxt = locate<ST, THREADS>(p, pre, per, all, x, false, &place);   // of the step to look up; it is STAGES + 1 ahead
     nxt.u = nxt.u * lines + line;
     int32_t ahead = p.a.lens[request_after(p, nxt.r)];
-    int32_t cur_r = nxt.r, cur_u = nxt.u, cost = nxt.cost, left = nxt.left;   // of the step at hand
+    int32_t togo = static_cast<int32_t>(xe - place);   // places from the step to look up to the end of this run
+    int32_t steps = 0;             // of this run, as far as they have been looked up
+    place += line0;
+    int32_t cur_r = nxt.r, cur_u = nxt.u, of_unit = nxt.steps, left = nxt.left;   // of the step at hand
     Heads hc = heads_of<NT>(p, cur_u);
     int32_t kv_up = hc.kv, kv_ask = hc.kv;   // kv heads of the step to look up, of the one to ask for
-    int32_t j_up = (cost - left) * ST + (lane & (ST - 1));   // this lane's token of the step to look up
+    int32_t j_up = (of_unit - left) * ST + (lane & (ST - 1));   // this lane's token of the step to look up
     const int32_t* table = p.a.tables + nxt.r * p.a.table_stride;
     int in = 0, out = 0;                     // places in to_come
-    bool whole = left == cost;               // the unit at hand began in this run
+    bool whole = left == of_unit;               // the unit at hand began in this run
     bool fresh = true;
     // Where this lane's chunks go: token k * RPI + lane / LPR, swizzled so that eight rows' chunks lie in different banks.
     const uint32_t ring_at = ptx::smem_u32(ring), chunk_l = lane % S::LPR, hi = lane / S::LPR;
@@ -337,7 +360,7 @@ paged_attention(const __grid_constant__ Params p) {
     int slot = 0;
 
 #pragma unroll 1
-    for (int32_t i = -STAGES - 1; i < steps; ++i) {
+    for (int32_t i = -STAGES - 1; i < steps || i < 0; ++i) {
       // ---- step i + STAGES: its page ids have come; rows of its tokens, a token per lane (or two)
       const bool ask = i >= -STAGES && i + STAGES < steps;
       if (ask) {
@@ -352,18 +375,21 @@ paged_attention(const __grid_constant__ Params p) {
         }
       }
       // ---- step i + STAGES + 1: look up the page ids
-      if (i + STAGES + 1 < steps) {
-        if (i > -STAGES - 1) {
-          j_up += ST;
-          if (--nxt.left == 0) {
-            next_unit<ST>(p, nxt, ahead, lines);
-            if (lane < 3) to_come[warp][in][lane] = lane == 0 ? nxt.r : lane == 1 ? nxt.u : nxt.cost;
-            in = (in + 1) & 3;   // (at most STAGES + 1 of them are waiting)
-            kv_up = heads_of<NT>(p, nxt.u).kv;
-            j_up = lane & (ST - 1);
-            table = p.a.tables + nxt.r * p.a.table_stride;
-          }
+      if (i > -STAGES - 1 && togo > 0) {
+        j_up += ST;
+        --togo;
+        if (--nxt.left == 0) {
+          --togo;
+          next_unit<ST>(p, nxt, ahead, lines);
+          if (lane < 3) to_come[warp][in][lane] = lane == 0 ? nxt.r : lane == 1 ? nxt.u : nxt.steps;
+          in = (in + 1) & 3;   // (at most STAGES + 1 of them are waiting)
+          kv_up = heads_of<NT>(p, nxt.u).kv;
+          j_up = lane & (ST - 1);
+          table = p.a.tables + nxt.r * p.a.table_stride;
         }
+      }
+      if (togo > 0) {
+        ++steps;
 #pragma unroll
         for (int k = 0; k < S::RL; ++k) {
           const int32_t j = j_up + 32 * k;
@@ -616,16 +642,21 @@ paged_attention(const __grid_constant__ Params p) {
       copies_commit();
       if (++slot == STAGES) slot = 0;
 
-      // ---- does the unit end here, or this warp's part of it?
+      // ---- does the unit end here, or this warp's part of it?  (What will be looked up has been: that is ahead.)
       if (i < -1) continue;
-      const bool over = i >= 0 && --left == 0, ends = over || i + 1 == steps;
-      if (!ends && i >= 0) continue;
-      const int32_t was_r = cur_r, was_u = cur_u, was_cost = cost, was_done = cost - left;
+      const bool over = i >= 0 && --left == 0, ends = i >= 0 && (over || i + 1 == steps);
+      if (!ends && i >= 0) {
+        ++place;
+        continue;
+      }
+      const int32_t was_r = cur_r, was_u = cur_u, was_steps = of_unit;
+      const int64_t was_start = place - (of_unit - left - 1);
       const Heads hw = hc;
       if (over && i + 1 < steps) {
+        place += 2;
         cur_r = to_come[warp][out][0];
         cur_u = to_come[warp][out][1];
-        cost = left = to_come[warp][out][2];
+        of_unit = left = to_come[warp][out][2];
         out = (out + 1) & 3;
         hc = heads_of<NT>(p, cur_u);
       }
@@ -703,7 +734,7 @@ paged_attention(const __grid_constant__ Params p) {
                   rows[q * PADDED + m * 16 + (E4 ? 2 * g + h : 8 * h + g)] = o[nt][m][2 * h + e] * f[nt][e];
               if (g == 0) plse[which][q] = sum[nt][e];
             }
-          if (lane == 0) piece[which] = Piece{was_r, was_u, was_cost, x + i + 1 - was_done};
+          if (lane == 0) piece[which] = Piece{was_r, was_u, was_steps, was_start};
         }
         whole = true;
       }
@@ -727,12 +758,12 @@ paged_attention(const __grid_constant__ Params p) {
     if (start) {
       const Piece u = piece[lane];
       group_at[__popc(starts & ((1u << lane) - 1))] = __popc(below);
-      if (u.start < a0 || u.start + u.cost > a1) {
+      if (u.start < a0 || u.start + u.steps > a1) {
         const int side = u.start < a0 ? 0 : 1;
         split[side] = u;
         const int k = static_cast<int>(quotient(u.start - line0, chunk));
         first[side] = k * lines + line;   // the CTA that the unit begins in
-        count[side] = static_cast<int>(quotient(u.start + u.cost - 1 - line0, chunk)) - k + 1;
+        count[side] = static_cast<int>(quotient(u.start + u.steps - 1 - line0, chunk)) - k + 1;
       }
     }
     if (lane == 0) {
@@ -763,7 +794,7 @@ paged_attention(const __grid_constant__ Params p) {
     }
     Lane<D>::scale(v, l == 0.f ? 0.f : __fdividef(1.f, l));
     l = l == 0.f ? -INFINITY : m + __log2f(l);
-    if (u.start >= a0 && u.start + u.cost <= a1) {
+    if (u.start >= a0 && u.start + u.steps <= a1) {
       const int64_t at = static_cast<int64_t>(u.r) * p.a.n_heads + h.first + q;
       Lane<D>::template store<QBF>(p.a.O, at * D, lane, v);
       if (lane == 0 && p.a.lse) p.a.lse[at] = l * kLn2;
