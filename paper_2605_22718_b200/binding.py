@@ -1,4 +1,5 @@
-"""ctypes binding of libworldkv.so: the same calls as include/wk.h, argument marshalling only.
+"""ctypes binding of libworldkv.so: the same calls as include/wk.h, argument marshalling only (that of the token-level cache's
+calls, which a program makes for every token, is compiled: csrc/pages_binding.cc).
 
 PyTorch supplies device memory and streams; every step of the path runs in the library's kernels.
 There is no fallback: if the shared library is missing or no sm_100 device is present, loading or
@@ -372,9 +373,9 @@ class PagedKV:
                  K_exp: Optional[torch.Tensor] = None, V_exp: Optional[torch.Tensor] = None,
                  n_pages: Optional[int] = None, page_tokens: Optional[int] = None):
         self.kv, self.lib, self.device = kv, kv.lib, kv.device
-        self._index = kv.device.index
+        self._index, self._native = kv.device.index, _pages()
         self.K, self.V, self.K_exp, self.V_exp = K, V, K_exp, V_exp
-        self._desc = None
+        self._desc, self._desc_at = None, 0
         if K is None:
             _need(n_pages is not None and page_tokens is not None, "PagedKV: K and V, or n_pages and page_tokens")
             self.n_pages, self.page_tokens = n_pages, page_tokens
@@ -410,9 +411,6 @@ class PagedKV:
         for x in tensors:
             _need(x is None or (x.is_cuda and x.get_device() == self._index), what + ": tensors on the context's device")
 
-    def _stream(self, stream) -> int:
-        return stream.cuda_stream if stream else torch._C._cuda_getCurrentRawStream(self._index)
-
     def free_pages(self) -> Tuple[torch.Tensor, torch.Tensor]:
         """(ring, state) for page_plan with every page free."""
         ring = torch.arange(self.n_pages, dtype=torch.int32, device=self.device)
@@ -424,48 +422,19 @@ class PagedKV:
                   starts_out: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
         """Pages and slots for the next step's tokens; lens and state are advanced in place unless lens_out, state_out are
         given.  Returns (slots [max_tokens], starts [n_req + 1]) int32, on the device."""
-        dev, n = self._index, lens.numel()
-        if lens_out is None:
-            lens_out = lens
-        elif not _ints(lens_out, n, dev):
-            raise WkError(WK_ERR_ARG, "wk_page_plan: lens_out [n_req] int32")
-        if state_out is None:
-            state_out = state
-        elif not _ints(state_out, 4, dev):
-            raise WkError(WK_ERR_ARG, "wk_page_plan: state_out [4] int32")
-        if not (_ints(lens, n, dev) and _ints(new_tokens, n, dev) and _ints(ring, self.n_pages, dev) and _ints(state, 4, dev)):
-            raise WkError(WK_ERR_ARG, "wk_page_plan: lens, new_tokens [n_req], ring [n_pages], state [4] int32, on the context's device")
-        rows, max_pages = _table(tables, n, dev, "wk_page_plan")
-        if slots_out is None:
-            slots_out = lens.new_empty(max_tokens)
-        elif not _ints(slots_out, max_tokens, dev):
-            raise WkError(WK_ERR_ARG, "wk_page_plan: slots_out [max_tokens] int32")
-        if starts_out is None:
-            starts_out = lens.new_empty(n + 1)
-        elif not _ints(starts_out, n + 1, dev):
-            raise WkError(WK_ERR_ARG, "wk_page_plan: starts_out [n_req + 1] int32")
-        st = self.lib.wk_page_plan(self.kv.ctx, self.n_pages, self.page_tokens, n, lens.data_ptr(), new_tokens.data_ptr(),
-                                   lens_out.data_ptr(), tables.data_ptr(), max_pages, rows, ring.data_ptr(),
-                                   state.data_ptr(), state_out.data_ptr(), max_tokens, slots_out.data_ptr(),
-                                   starts_out.data_ptr(), self._stream(stream))
-        if st != WK_OK:
-            raise WkError(st, "wk_page_plan")
-        return slots_out, starts_out
+        kv = self.kv
+        r = self._native.page_plan(kv.ctx.value if kv.ctx else 0, self._index, self.n_pages, self.page_tokens, lens, new_tokens,
+                                   lens_out, tables, ring, state, state_out, max_tokens, slots_out, starts_out,
+                                   stream.cuda_stream if stream else None)
+        return r if r.__class__ is tuple else _failed(r, "wk_page_plan", kv)
 
     def page_store(self, K_new: torch.Tensor, V_new: torch.Tensor, slots: torch.Tensor, stream=None) -> None:
         """Rows K_new, V_new [n, n_kv_heads, head_dim] (heads contiguous, any row stride, both alike) into slots [>= n]."""
-        dev, shape, strides, dtype = self._index, K_new.shape, K_new.stride(), K_new.dtype
-        if not (self._desc is not None and len(shape) == 3 and shape[1] == self.n_kv_heads and shape[2] == self.head_dim
-                and V_new.shape == shape and V_new.stride() == strides and V_new.dtype is dtype and dtype in _TYPES
-                and strides[2] == 1 and (strides[1] == shape[2] or shape[1] == 1)
-                and K_new.get_device() == dev and V_new.get_device() == dev):
-            raise WkError(WK_ERR_ARG, "wk_page_store: K_new, V_new [n, n_kv_heads, head_dim] alike, heads contiguous")
-        if not _ints(slots, shape[0], dev):
-            raise WkError(WK_ERR_ARG, "wk_page_store: slots int32")
-        st = self.lib.wk_page_store(self.kv.ctx, self._desc_at, K_new.data_ptr(), V_new.data_ptr(), _TYPES[dtype], shape[0],
-                                    strides[0], slots.data_ptr(), self._stream(stream))
-        if st != WK_OK:
-            raise WkError(st, "wk_page_store")
+        kv = self.kv
+        r = self._native.page_store(kv.ctx.value if kv.ctx else 0, self._index, self._desc_at, K_new, V_new, slots,
+                                    stream.cuda_stream if stream else None)
+        if r is not None:
+            _failed(r, "wk_page_store", kv)
 
     def paged_attention(self, Q: torch.Tensor, tables: torch.Tensor, lens: torch.Tensor, window: int = 0, sink: int = 0,
                         softmax_scale: float = 0.0, O: Optional[torch.Tensor] = None, lse_out: Optional[torch.Tensor] = None,
@@ -473,31 +442,11 @@ class PagedKV:
         """O [n_req, n_heads, head_dim] of one new token per request: Q [n_req, n_heads, head_dim] (heads contiguous, any
         row stride) over the tokens that tables and lens name.  scratch: as WorldKV's, shared by the calls of a context unless
         given (zero-filled once; for calls that may overlap on the GPU)."""
-        dev, shape, strides, dtype = self._index, Q.shape, Q.stride(), Q.dtype
-        if not (self._desc is not None and len(shape) == 3 and shape[2] == self.head_dim and dtype in _TYPES and strides[2] == 1
-                and (strides[1] == shape[2] or shape[1] == 1) and Q.get_device() == dev):
-            raise WkError(WK_ERR_ARG, "wk_paged_attention: Q [n_req, n_heads, head_dim], heads contiguous")
-        n, heads, d = shape
-        if not _ints(lens, n, dev):
-            raise WkError(WK_ERR_ARG, "wk_paged_attention: lens [n_req] int32")
-        rows, max_pages = _table(tables, n, dev, "wk_paged_attention")
-        if O is None:
-            O = torch.empty_like(Q) if Q.is_contiguous() else Q.new_empty(shape)
-        elif not (O.shape == shape and O.dtype is dtype and O.is_contiguous() and O.get_device() == dev):
-            raise WkError(WK_ERR_ARG, "wk_paged_attention: O like Q, contiguous")
-        if lse_out is not None and not (lse_out.shape == shape[:2] and lse_out.dtype is torch.float32
-                                        and lse_out.is_contiguous() and lse_out.get_device() == dev):
-            raise WkError(WK_ERR_ARG, "wk_paged_attention: lse_out [n_req, n_heads] fp32")
-        if scratch is None:
-            scratch = self.kv.paged_scratch
-        if n == 0:
-            return O
-        st = self.lib.wk_paged_attention(self.kv.ctx, self._desc_at, Q.data_ptr(), _TYPES[dtype], strides[0], n, heads,
-                                         tables.data_ptr(), max_pages, rows, lens.data_ptr(), window, sink, softmax_scale,
-                                         O.data_ptr(), _ptr(lse_out), scratch.data_ptr(), scratch.numel(), self._stream(stream))
-        if st != WK_OK:
-            raise WkError(st, f"wk_paged_attention (last CUDA error {self.kv.last_cuda_error()})")
-        return O
+        kv = self.kv
+        r = self._native.paged_attention(kv.ctx.value if kv.ctx else 0, self._index, self._desc_at, Q, tables, lens, window, sink,
+                                         softmax_scale, O, lse_out, scratch if scratch is not None else kv.paged_scratch,
+                                         stream.cuda_stream if stream else None)
+        return r if r.__class__ is not int and r.__class__ is not str else _failed(r, "wk_paged_attention", kv)
 
 
 def _need(ok: bool, what: str) -> None:
@@ -505,13 +454,26 @@ def _need(ok: bool, what: str) -> None:
         raise WkError(WK_ERR_ARG, what)
 
 
-def _ints(x: torch.Tensor, size: int, device: int) -> bool:
-    return x.dtype is torch.int32 and x.numel() >= size and x.is_contiguous() and x.get_device() == device
+def _failed(r, what: str, kv: WorldKV):
+    """Raises for what the marshalling returned in place of tensors: what is wrong with an argument, or a call's status."""
+    if isinstance(r, str):
+        raise WkError(WK_ERR_ARG, r)
+    raise WkError(r, f"{what} (last CUDA error {kv.last_cuda_error() if kv.ctx else 0})")
 
 
-def _table(tables: torch.Tensor, n: int, device: int, what: str) -> Tuple[int, int]:
-    """(row stride, columns) of block tables [>= n, max_pages]."""
-    shape, strides = tables.shape, tables.stride()
-    if not (tables.dtype is torch.int32 and len(shape) == 2 and shape[0] >= n and strides[1] == 1 and tables.get_device() == device):
-        raise WkError(WK_ERR_ARG, what + ": tables [n_req, max_pages] int32")
-    return strides[0], shape[1]
+_marshalling = None
+
+
+def _pages():
+    """The compiled marshalling of the three calls (csrc/pages_binding.cc), told where the library has them."""
+    global _marshalling
+    if _marshalling is None:
+        lib = load_library()
+        try:
+            from . import _pages as native
+        except ImportError as e:
+            raise RuntimeError("_pages.so is missing or does not fit this PyTorch: run `python -m paper_2605_22718_b200.build`; "
+                               "there is no fallback path") from e
+        native.use(*[C.cast(f, C.c_void_p).value for f in (lib.wk_page_plan, lib.wk_page_store, lib.wk_paged_attention)])
+        _marshalling = native
+    return _marshalling

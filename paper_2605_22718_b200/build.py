@@ -2,9 +2,10 @@
 
 ``build_all()`` compiles
   * ``paper_2605_22718_b200/libworldkv.so``  -- the product: the C-ABI library declared in include/wk.h
+  * ``paper_2605_22718_b200/_pages.so``      -- argument marshalling of the token-level cache's calls (g++, PyTorch's headers)
   * ``wkinputs/libwkinputs.so``              -- the seeded input generators' device side
   * ``tests/cuda/libwk_wait_probe.so``       -- test-only: the product's bounded mbarrier wait built with a small cap
-with nvcc.  nvcc cross-compiles without a GPU, so this also runs on a CPU-only machine.
+with nvcc and g++.  nvcc cross-compiles without a GPU, so this also runs on a CPU-only machine.
 """
 from __future__ import annotations
 
@@ -12,10 +13,12 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 CSRC = os.path.join(ROOT, "paper_2605_22718_b200", "csrc")
 LIB_WORLDKV = os.path.join(ROOT, "paper_2605_22718_b200", "libworldkv.so")
+LIB_PAGES = os.path.join(ROOT, "paper_2605_22718_b200", "_pages.so")
 LIB_INPUTS = os.path.join(ROOT, "wkinputs", "libwkinputs.so")
 LIB_WAIT_PROBE = os.path.join(ROOT, "tests", "cuda", "libwk_wait_probe.so")
 
@@ -45,7 +48,19 @@ def _run(cmd, log_name: str) -> None:
         f.write(" ".join(cmd) + "\n" + res.stdout)
     if res.returncode != 0:
         sys.stderr.write(res.stdout)
-        raise RuntimeError("nvcc failed: " + " ".join(cmd))
+        raise RuntimeError("the compiler failed: " + " ".join(cmd))
+
+
+def _host_command(source: str, target: str):
+    """g++ on a source that uses Python's and PyTorch's headers (both are loaded already where the target is imported)."""
+    import torch
+    at = os.path.dirname(torch.__file__)
+    cuda = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(_nvcc()))), "include")
+    includes = [sysconfig.get_paths()["include"], os.path.join(at, "include"), os.path.join(at, "include", "torch", "csrc", "api", "include"), cuda]
+    flags = [x for d in includes for x in ("-isystem", d)]
+    return ["g++", "-std=c++17", "-O2", "-shared", "-fPIC", "-fvisibility=hidden",
+            "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI, *flags, "-o", target, source, "-L", os.path.join(at, "lib"),
+            "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
 
 
 def build_all(force: bool = False) -> None:
@@ -54,6 +69,9 @@ def build_all(force: bool = False) -> None:
         os.path.join(ROOT, "include", "wk.h")]
     if force or _stale(LIB_WORLDKV, deps):
         _run([_nvcc()] + NVCC_FLAGS + ["-I", os.path.join(ROOT, "include"), "-o", LIB_WORLDKV] + srcs, "libworldkv.log")
+    marshalling = os.path.join(CSRC, "pages_binding.cc")
+    if force or _stale(LIB_PAGES, [marshalling, os.path.join(ROOT, "include", "wk.h")]):
+        _run(_host_command(marshalling, LIB_PAGES), "_pages.log")
     gen = os.path.join(ROOT, "wkinputs", "gen.cu")
     if force or _stale(LIB_INPUTS, [gen]):
         _run([_nvcc()] + NVCC_FLAGS + ["-o", LIB_INPUTS, gen], "libwkinputs.log")
