@@ -256,3 +256,42 @@ def test_refusals(kv):
             c.paged_attention(*args, **kw)
         assert e.value.status in (status, WK_ERR_ARG), (args, kw)
     assert c.paged_attention(Q[:0], tables[:0], lens[:0]).shape == (0, 12, 128)
+
+
+@pytest.mark.parametrize("type_,d,heads,kv_heads,lens,window,sink", [
+    ("e4m3", 128, 16, 8, [90000, 41111, 1, 0, 7000], 0, 0),          # neighbouring heads side by side, runs of a few hundred steps
+    ("e4m3", 128, 12, 12, [60001, 33333], 0, 0),
+    ("e4m3", 64, 5, 5, [400000], 0, 0),
+    ("f16", 64, 40, 40, [9999, 20000, 5, 8192], 0, 0),               # five heads one after the other on each of eight lines
+    ("bf16", 128, 80, 4, [50000, 20003], 0, 0),                      # two units share every kv head
+    ("bf16", 128, 66, 2, [100001, 0, 30], 0, 0),                     # three do
+    ("e4m3", 128, 8, 8, [150000, 90000], 100000, 77),
+])
+def test_long_runs(kv, type_, d, heads, kv_heads, lens, window, sink):
+    check(kv, setup(type_, lens, heads, kv_heads, d, 64, seed=3, window=window, sink=sink, dirty=False), window=window, sink=sink)
+
+
+@pytest.mark.parametrize("type_,d,heads,kv_heads,lens", [
+    ("f16", 64, 32, 8, [55] * 20), ("e4m3", 64, 8, 8, [205] * 31), ("bf16", 128, 4, 4, [1] * 37), ("bf16", 128, 8, 2, [128, 0, 1, 129, 16, 17] * 9),
+    ("bf16", 128, 4, 1, [120, 136, 8] * 40), ("e4m3", 128, 16, 16, [256, 257, 31] * 11), ("f16", 64, 3, 3, [300] * 77), ("bf16", 64, 20, 1, [90] * 16),
+])
+def test_short_runs(kv, type_, d, heads, kv_heads, lens):
+    """So little work that every warp has a few steps: CTAs begin and end with short units."""
+    check(kv, setup(type_, lens, heads, kv_heads, d, 16, seed=len(lens)))
+
+
+def test_a_short_run_beside_rows_that_do_not_exist(kv):
+    lens = ([-1, 40, 0, 17, -1] * 12) + [-1] * 300
+    K, V, ke, ve, tables, dev, Q = setup("bf16", lens, 8, 4, 128, 16)
+    O, lse = call(kv, K, V, ke, ve, tables, dev, Q)
+    there = dev >= 0
+    assert (O[~there] == 55).all() and (lse[~there] == 77).all()
+    lib.assert_attends(O[there], lse[there], [x[there] for x in lib.attend(Q, K, V, ke, ve, tables, lens)])
+
+
+def test_an_output_of_a_tensor_subclass(kv):
+    from paper_2605_22718_b200 import PagedKV
+    K, V, _, _, tables, lens, Q = setup("bf16", [33], 4, 4, 128, 16)
+    O = torch.nn.Parameter(torch.empty_like(Q), requires_grad=False)
+    assert PagedKV(kv, K, V).paged_attention(Q, tables, lens, O=O) is O
+    assert torch.equal(O, PagedKV(kv, K, V).paged_attention(torch.nn.Parameter(Q, requires_grad=False), tables, lens))
