@@ -337,8 +337,8 @@ size_t wk_paged_scratch_bytes(const wk_ctx* ctx);
  *             -inf) is O = 0, lse = -inf; a logit that is NaN or +inf makes its row NaN
  *   softmax_scale 0 selects 1/sqrt(head_dim); window 0: all tokens
  *   scratch   wk_paged_scratch_bytes() bytes, 256-byte aligned
- * Errors: WK_ERR_SHAPE (n_heads not a multiple of n_kv_heads, scratch too small, a cache of 64 GB or more,
- * tables that name 2^31 * 16 tokens or more), WK_ERR_ARG. */
+ * Errors: WK_ERR_SHAPE (n_heads not a multiple of n_kv_heads, scratch too small, a cache of 64 GB or more),
+ * WK_ERR_ARG. */
 wk_status wk_paged_attention(wk_ctx* ctx, const wk_paged_kv* cache, const void* Q, int32_t q_type, int64_t q_stride,
                              int32_t n_req, int32_t n_heads, const int32_t* tables, int32_t max_pages,
                              int64_t table_stride, const int32_t* lens, int32_t window, int32_t sink,

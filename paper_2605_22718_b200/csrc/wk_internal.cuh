@@ -204,6 +204,20 @@ wk_status launch_attention(wk_ctx* ctx, int layer, const __nv_bfloat16* Q, int l
 wk_status launch_retrieve_query(wk_ctx* ctx, int layer, const __nv_bfloat16* Q, int lq, int k, int32_t* slots_out,
                                 float* score_out, cudaStream_t s);
 
+// x / d by a multiplication, for x < 2^31: with l the least power for which 2^l >= d, 2^(31 + l) / d rounded up errs by less than
+// 2^l / 2^(31 + l) per unit of x.
+struct Divisor {
+  uint32_t mul, shift;
+#ifdef __CUDACC__
+  __device__ __forceinline__ uint32_t quotient(uint32_t x) const { return static_cast<uint32_t>(static_cast<uint64_t>(x) * mul >> shift); }
+#endif
+};
+inline Divisor divisor(uint32_t d) {
+  uint32_t l = 0;
+  while ((1ull << l) < d) ++l;
+  return {static_cast<uint32_t>(((1ull << (31 + l)) + d - 1) / d), 31 + l};
+}
+
 // Token-level cache in pages (entry points in wk_paged_api.cu).
 constexpr int kPlanMaxReq = 4096;   // four for each of 1,024 threads
 struct PlanArgs {
@@ -236,6 +250,8 @@ struct PagedArgs {
   uint8_t* scratch;
   uint32_t* status;
 };
+// The query heads of a kv head are taken 8 at a time, or 16 where there are more.
+inline int paged_query_tiles(int group) { return group > 8 ? (group + 15) / 16 : 1; }
 wk_status launch_paged_attention(wk_ctx* ctx, const PagedArgs& a, cudaStream_t s);
 size_t paged_scratch_bytes(int sm_count);
 

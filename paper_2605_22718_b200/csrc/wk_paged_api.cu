@@ -97,8 +97,6 @@ wk_status wk_paged_attention(wk_ctx* ctx, const wk_paged_kv* cache, const void* 
   if (reach >= 4294967295.0) return WK_ERR_SHAPE;
   // positions are 32-bit; a table longer than that cannot be used to its end
   const int64_t room = 0x7fffffffLL / cache->page_tokens;
-  // ... and the steps of all requests, 16 tokens or more each
-  if ((static_cast<int64_t>(max_pages < room ? max_pages : room) * cache->page_tokens / 16 + 2) * n_req > 0x7fffffffLL) return WK_ERR_SHAPE;
   WK_USE_DEVICE(ctx);
   PagedArgs a;
   a.c = *cache;

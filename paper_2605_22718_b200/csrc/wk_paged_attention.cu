@@ -26,6 +26,8 @@
 //     scratch buffer; the CTA that arrives last joins them in their order, so that the result does not depend on the arrival.
 #include <cuda_fp16.h>
 
+#include <algorithm>
+
 #include "ptx_sm100.cuh"
 #include "wk_internal.cuh"
 
@@ -35,7 +37,6 @@ namespace {
 constexpr uint32_t kNowhere = 0xffffffffu;   // row offset of a token that is not attended
 constexpr float kLazy = 8.f;                 // how far (log2) a logit may exceed the reference
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
-constexpr int kStepBytes = 8192;             // of K and V in a step
 constexpr int kShortRun = 4, kWhole = 8;     // where runs are that short, CTAs go round units of up to so many steps
 constexpr int kLongRun = 24;                 // steps per warp from which on heads are walked side by side
 
@@ -47,7 +48,7 @@ struct Params {
   uint32_t page16, token16;        // strides in units of 16 bytes
   int64_t head_bytes;              // stride of a kv head
   int32_t counter_bytes;           // of the scratch buffer, before the pieces
-  uint32_t page_mul, page_shift;   // pos / page_tokens = pos * page_mul >> page_shift for pos < 2^31
+  Divisor by_page, by_workers[2];  // by the warps that share a line: of one, of `lines`
 };
 
 template <int MODE, int D, int NT>
@@ -58,7 +59,9 @@ struct Shape {
   static constexpr int STAGES = 2;
   static constexpr int ES = MODE == WK_E4M3 ? 1 : 2;     // bytes per element of the cache
   static constexpr int ROW = D * ES;                     // bytes of a row
-  static constexpr int ST = kStepBytes / 2 / ROW;        // tokens of a step: 16, 32 or 64
+  static constexpr int STEP = 8192;                      // bytes of K and V in a step
+  static constexpr int COPIES = STEP / 1024;             // copy instructions for a step's K, as many for its V
+  static constexpr int ST = STEP / 2 / ROW;              // tokens of a step: 16, 32 or 64
   static constexpr int RL = ST > 32 ? ST / 32 : 1;       // tokens per lane when rows are looked up
   static constexpr int LPR = ROW / 16;                   // lanes (16-byte chunks) per row
   static constexpr int RPI = 32 / LPR;                   // rows per copy instruction
@@ -153,12 +156,6 @@ __device__ __forceinline__ int32_t measure(const Params& p, int32_t len, int32_t
   return *shown > ST ? static_cast<int32_t>((static_cast<uint32_t>(*shown) + ST - 1) / ST) : 1;
 }
 
-// a / b of numbers that hardly ever need 64 bits
-__device__ __noinline__ int64_t quotient64(int64_t a, int64_t b) { return a / b; }
-__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
-  return (a | b) >> 32 ? quotient64(a, b) : static_cast<int64_t>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b));
-}
-
 __device__ __forceinline__ uint32_t places(int32_t steps) { return steps ? steps + 1u : 0u; }
 
 __device__ __forceinline__ int32_t request_after(const Params& p, int32_t r) { return r + 1 == p.a.n_req ? 0 : r + 1; }
@@ -181,10 +178,10 @@ __device__ __forceinline__ void next_unit(const Params& p, Unit& v, int32_t& ahe
 // steps, the unit's first step or the next unit's, whichever is nearer (only the place is told then).
 // *at: that step's place.  u: counted in the line.  pre[t]: places of the requests before thread t's `per` requests, of all: `all`.
 template <int ST, int THREADS>
-__device__ __forceinline__ Unit locate(const Params& p, const uint32_t* pre, int per, uint32_t all, int64_t x, bool uncut, int64_t* at) {
+__device__ __forceinline__ Unit locate(const Params& p, const uint32_t* pre, int per, uint32_t all, uint32_t x, bool uncut, int32_t* at) {
   Unit v;
-  v.u = static_cast<int32_t>(quotient(x, all));
-  const uint32_t z = static_cast<uint32_t>(x - static_cast<int64_t>(v.u) * all);
+  v.u = x < all ? 0 : x / all;
+  const uint32_t z = x - v.u * all;
   int lo = -1;   // (the whole warp is here)
 #pragma unroll
   for (int k = 0; k < THREADS; k += 32) lo += __popc(__ballot_sync(0xffffffffu, pre[k + (threadIdx.x & 31)] <= z));
@@ -200,7 +197,7 @@ __device__ __forceinline__ Unit locate(const Params& p, const uint32_t* pre, int
   v.steps = max(v.steps, 1);
   int32_t step = max(static_cast<int32_t>(z - before) - 1, 0);
   if (uncut && v.steps <= kWhole) step = 2 * (z - before) >= places(v.steps) ? v.steps + 1 : 0;
-  *at = static_cast<int64_t>(v.u) * all + before + 1 + step;
+  *at = v.u * all + before + 1 + step;
   v.left = v.steps - step;
   return v;
 }
@@ -221,7 +218,7 @@ __device__ __forceinline__ Heads heads_of(const Params& p, int u) {
 // What the warps and CTAs that share a unit leave each other.
 struct Piece {
   int32_t r, u, steps;  // r < 0: none
-  int64_t start;        // place of the unit's first step
+  int32_t start;        // place of the unit's first step
 };
 constexpr int kPieceFloats = 16 * (128 + 1);   // of a piece in the scratch buffer: log-sum-exps, then rows
 constexpr size_t counter_bytes(int ctas) { return (ctas * sizeof(uint32_t) + 255) / 256 * 256; }
@@ -267,12 +264,12 @@ paged_attention(const __grid_constant__ Params p) {
   __shared__ int32_t to_come[W][4][3];   // units that the walk ahead has entered: request, unit, steps
   __shared__ int32_t first[2], count[2], n_groups, group_at[2 * W + 1], order[2 * W];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
-  uint8_t* const ring = dyn + warp * (STAGES * kStepBytes);
-  uint8_t* const firsts = dyn + W * (STAGES * kStepBytes);
+  uint8_t* const ring = dyn + warp * (STAGES * S::STEP);
+  uint8_t* const firsts = dyn + W * (STAGES * S::STEP);
   uint8_t* const exps = firsts + W * S::PIECE + warp * (STAGES * S::META);
   // piece i of the CTA (warp i / 2's first or last)
   auto piece_rows = [&](int i) -> float* {
-    return reinterpret_cast<float*>(i & 1 ? dyn + (i >> 1) * (STAGES * kStepBytes) : firsts + (i >> 1) * S::PIECE);
+    return reinterpret_cast<float*>(i & 1 ? dyn + (i >> 1) * (STAGES * S::STEP) : firsts + (i >> 1) * S::PIECE);
   };
 
   // (launched while the kernel before it drains, and the one behind it likewise: nothing is read or written before this)
@@ -308,25 +305,27 @@ paged_attention(const __grid_constant__ Params p) {
   pre[tid] = before + up - mine;
   __syncthreads();
   // CTA k * lines + line takes the k-th run of a line; for short runs side by side is not worth the SMs that are left over.
-  const int lines = p.lines > 1 && static_cast<int64_t>(all) * p.units >= kLongRun * static_cast<int64_t>(gridDim.x * W) ? p.lines : 1;
+  const uint32_t total = all * p.units;   // (the host has seen to it that places have 31 bits)
+  const int lines = p.lines > 1 && total >= kLongRun * gridDim.x * W ? p.lines : 1;
   const int line = lines == 1 ? 0 : blockIdx.x % lines, column = lines == 1 ? blockIdx.x : blockIdx.x / lines;
-  const int64_t length = static_cast<int64_t>(all) * (lines == 1 ? p.units : p.units / lines), line0 = line * length;
+  const int32_t length = lines == 1 ? total : total / lines, line0 = line * length;
+  const Divisor by_workers = p.by_workers[lines > 1];
   const uint32_t workers = (lines == 1 ? gridDim.x : gridDim.x / lines) * W;
-  int64_t run = quotient(length + workers - 1, workers);
-  const int64_t chunk = run * W;
+  int32_t run = by_workers.quotient(length + workers - 1);
+  const int32_t chunk = run * W;
   if (column * chunk >= length) return;
   if (lane < 2) piece[2 * warp + lane].r = -1;
   // Short runs of short units: a CTA's run begins and ends with a unit, for a join of CTAs costs more than a few steps (20 requests of 55 tokens,
   // 8 heads of 64: 8.7 us -> 7.0; where runs are longer, cuts anywhere balance them: 256 requests of up to 300 tokens, 16 heads of 64, 21.2 us,
   // 23.2 if they went round units).
-  int64_t a0 = column * chunk, a1 = min(a0 + chunk, length);
+  int32_t a0 = column * chunk, a1 = min(a0 + chunk, length);
   if (run <= kShortRun && all <= 2u * kWhole * p.a.n_req) {
-    const int64_t from = a0, to = a1;
+    const int32_t from = a0, to = a1;
     if (from > 0) locate<ST, THREADS>(p, pre, per, all, from, true, &a0);
     if (to < length) locate<ST, THREADS>(p, pre, per, all, to, true, &a1);
-    run = max(a1 - a0 + W - 1, static_cast<int64_t>(0)) / W;
+    run = max(a1 - a0 + W - 1, 0) / W;
   }
-  const int64_t x = a0 + warp * run, xe = min(x + run, a1);
+  const int32_t x = a0 + warp * run, xe = min(x + run, a1);
   a0 += line0;
   a1 += line0;
 
@@ -338,11 +337,11 @@ paged_attention(const __grid_constant__ Params p) {
     float sc[NT][2];               // logit scale of query heads 2c, 2c + 1
     float ref[NT][2], refw[NT][2]; // references of the sum and (8 bits) of the weights
     float sum[NT][2], o[NT][MT][4];
-    int64_t place;                 // of the step at hand
+    int32_t place;                 // of the step at hand
     Unit nxt = locate<ST, THREADS>(p, pre, per, all, x, false, &place);   // of the step to look up; it is STAGES + 1 ahead
     nxt.u = nxt.u * lines + line;
     int32_t ahead = p.a.lens[request_after(p, nxt.r)];
-    int32_t togo = static_cast<int32_t>(xe - place);   // places from the step to look up to the end of this run
+    int32_t togo = xe - place;   // places from the step to look up to the end of this run
     int32_t steps = 0;             // of this run, as far as they have been looked up
     place += line0;
     int32_t cur_r = nxt.r, cur_u = nxt.u, of_unit = nxt.steps, left = nxt.left;   // of the step at hand
@@ -396,7 +395,7 @@ paged_attention(const __grid_constant__ Params p) {
           id[k] = -1;
           if (j < nxt.shown) {
             const uint32_t pos = static_cast<uint32_t>(j >= p.a.sink ? j + nxt.shift : j);
-            const uint32_t at = static_cast<uint32_t>(static_cast<uint64_t>(pos) * p.page_mul >> p.page_shift);
+            const uint32_t at = p.by_page.quotient(pos);
             off[k] = pos - at * p.a.c.page_tokens;
             id[k] = __ldg(table + at);
           }
@@ -406,7 +405,7 @@ paged_attention(const __grid_constant__ Params p) {
       if (i >= 0) {
         copies_wait<STAGES - 1>();
         __syncwarp();
-        const uint32_t k_at = ring_at + slot * kStepBytes, v_at = k_at + kStepBytes / 2;
+        const uint32_t k_at = ring_at + slot * S::STEP, v_at = k_at + S::STEP / 2;
         if (fresh) {   // a unit begins: Q has been asked for
           fresh = false;
 #pragma unroll
@@ -612,16 +611,16 @@ paged_attention(const __grid_constant__ Params p) {
       // ---- ask for the rows just looked up, in the place of the step just used
       __syncwarp();
       if (ask) {
-        const uint32_t to = ring_at + slot * kStepBytes + to_l;
+        const uint32_t to = ring_at + slot * S::STEP + to_l;
         const char* const from = static_cast<const char*>(p.a.c.K) + kv_ask * p.head_bytes + chunk_l * 16;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-          const uint32_t at = __shfl_sync(0xffffffffu, row[S::RL == 1 || k < 4 ? 0 : S::RL - 1], (k * S::RPI + hi) & 31);
+        for (int k = 0; k < S::COPIES; ++k) {
+          const uint32_t at = __shfl_sync(0xffffffffu, row[k * S::RPI / 32], (k * S::RPI + hi) & 31);
           const bool skip = at == kNowhere;
           const char* const src = from + static_cast<uint64_t>(skip ? 0 : at) * 16;
           const uint32_t dst = (ROW == 64 ? to : to ^ ((k * S::RPI & 7) << 4)) + k * 512;
           copy16(dst, src, skip);
-          copy16(dst + kStepBytes / 2, src + v_minus_k, skip);
+          copy16(dst + S::STEP / 2, src + v_minus_k, skip);
         }
 #pragma unroll
         for (int k = 0; k < S::RL; ++k) {
@@ -650,7 +649,7 @@ paged_attention(const __grid_constant__ Params p) {
         continue;
       }
       const int32_t was_r = cur_r, was_u = cur_u, was_steps = of_unit;
-      const int64_t was_start = place - (of_unit - left - 1);
+      const int32_t was_start = place - (of_unit - left - 1);
       const Heads hw = hc;
       if (over && i + 1 < steps) {
         place += 2;
@@ -761,9 +760,9 @@ paged_attention(const __grid_constant__ Params p) {
       if (u.start < a0 || u.start + u.steps > a1) {
         const int side = u.start < a0 ? 0 : 1;
         split[side] = u;
-        const int k = static_cast<int>(quotient(u.start - line0, chunk));
+        const int k = static_cast<uint32_t>(u.start - line0) / static_cast<uint32_t>(chunk);
         first[side] = k * lines + line;   // the CTA that the unit begins in
-        count[side] = static_cast<int>(quotient(u.start + u.steps - 1 - line0, chunk)) - k + 1;
+        count[side] = static_cast<uint32_t>(u.start + u.steps - 1 - line0) / static_cast<uint32_t>(chunk) - k + 1;
       }
     }
     if (lane == 0) {
@@ -896,7 +895,7 @@ paged_attention(const __grid_constant__ Params p) {
 template <int MODE, int D, int NT, bool QBF>
 wk_status launch(wk_ctx* ctx, const Params& p, cudaStream_t s) {
   using S = Shape<MODE, D, NT>;
-  constexpr int smem = S::W * (S::STAGES * (kStepBytes + S::META) + S::PIECE);
+  constexpr int smem = S::W * (S::STAGES * (S::STEP + S::META) + S::PIECE);
   const int i = ((MODE * 2 + (D == 128)) * 2 + NT - 1) * 2 + QBF;
   if (!(ctx->paged_attr_set >> i & 1)) {
     WK_CUDA_TRY(ctx, cudaFuncSetAttribute(paged_attention<MODE, D, NT, QBF>, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
@@ -919,12 +918,12 @@ size_t paged_scratch_bytes(int sm_count) {
   return counter_bytes(sm_count) + static_cast<size_t>(2) * sm_count * kPieceFloats * sizeof(float);
 }
 
-wk_status launch_paged_attention(wk_ctx* ctx, const PagedArgs& a, cudaStream_t s) {
+static wk_status launch_requests(wk_ctx* ctx, const PagedArgs& a, int32_t room, cudaStream_t s) {
   Params p;
   p.a = a;
   p.group = a.n_heads / a.c.n_kv_heads;
   const int nt = p.group > 8 ? 2 : 1;
-  p.q_tiles = (p.group + 8 * nt - 1) / (8 * nt);
+  p.q_tiles = paged_query_tiles(p.group);
   p.units = a.c.n_kv_heads * p.q_tiles;
   const int es = a.c.type == WK_E4M3 ? 1 : 2;
   // Units of long requests are walked side by side, so that rows of neighbouring heads, neighbours in memory as a rule, are read at
@@ -935,19 +934,40 @@ wk_status launch_paged_attention(wk_ctx* ctx, const PagedArgs& a, cudaStream_t s
   if (a.c.head_dim * es < 256 || p.q_tiles > 1)
     for (int d = 2; d <= 16; ++d)
       if (p.units % d == 0 && ctx->sm_count / d * d >= ctx->sm_count - ctx->sm_count / 32) p.lines = d;
-  p.room = a.max_pages * a.c.page_tokens;
+  p.room = room;
   p.page16 = static_cast<uint32_t>(a.c.page_stride * es / 16);
   p.token16 = static_cast<uint32_t>(a.c.token_stride * es / 16);
   p.head_bytes = a.c.head_stride * es;
-  // with l the least power for which 2^l >= page: 2^(31 + l) / page, rounded up, errs by less than 2^l / 2^(31 + l) per position
-  uint32_t l = 0;
-  while ((1ull << l) < static_cast<uint64_t>(a.c.page_tokens)) ++l;
-  p.page_shift = 31 + l;
-  p.page_mul = static_cast<uint32_t>(((1ull << (31 + l)) + a.c.page_tokens - 1) / a.c.page_tokens);
+  p.by_page = divisor(a.c.page_tokens);
+  using S = Shape<WK_BF16, 128, 1>;   // (all shapes have as many warps)
+  p.by_workers[0] = divisor(ctx->sm_count * S::W);
+  p.by_workers[1] = divisor(ctx->sm_count / p.lines * S::W);
   p.counter_bytes = static_cast<int32_t>(counter_bytes(ctx->sm_count));
   if (a.c.type == WK_BF16) return choose<WK_BF16, true>(ctx, p, nt, s);
   if (a.c.type == WK_F16) return choose<WK_F16, false>(ctx, p, nt, s);
   return a.q_type == WK_BF16 ? choose<WK_E4M3, true>(ctx, p, nt, s) : choose<WK_E4M3, false>(ctx, p, nt, s);
+}
+
+wk_status launch_paged_attention(wk_ctx* ctx, const PagedArgs& a, cudaStream_t s) {
+  // The kernel counts places of its line in 31 bits.  What the lengths are only the GPU knows; where the tables have room for more
+  // than that, the requests are taken in several launches.  (For a single request it is 2^35 tokens over its kv heads, more than a
+  // cache of less than 64 GB holds.)
+  const int64_t units = static_cast<int64_t>(a.c.n_kv_heads) * paged_query_tiles(a.n_heads / a.c.n_kv_heads);
+  const int64_t most = 0x7fff0000LL / units;   // places of the requests of a launch, per unit
+  const int64_t room = std::min<int64_t>(static_cast<int64_t>(a.max_pages) * a.c.page_tokens, (most - 2) * 16);
+  const int64_t each = room / 16 + 2, some = std::max<int64_t>(std::min<int64_t>(a.n_req, most / each), 1);
+  for (int64_t r = 0; r < a.n_req; r += some) {
+    PagedArgs b = a;
+    b.n_req = static_cast<int32_t>(std::min<int64_t>(some, a.n_req - r));
+    b.Q = static_cast<const uint16_t*>(a.Q) + r * a.q_stride;
+    b.O = static_cast<uint16_t*>(a.O) + r * a.n_heads * a.c.head_dim;
+    b.lse = a.lse ? a.lse + r * a.n_heads : nullptr;
+    b.tables = a.tables + r * a.table_stride;
+    b.lens = a.lens + r;
+    const wk_status st = launch_requests(ctx, b, static_cast<int32_t>(room), s);
+    if (st != WK_OK) return st;
+  }
+  return WK_OK;
 }
 
 }  // namespace wk

@@ -261,18 +261,6 @@ page_plan(const __grid_constant__ PlanArgs a) {
 constexpr int kStoreThreads = 128;
 constexpr int kStoreLoads = 4;   // 16-byte loads in flight per thread
 
-// x / d by a multiplication, for x < 2^31: with l the least power for which 2^l >= d, 2^(31 + l) / d rounded up errs by less than
-// 2^l / 2^(31 + l) per unit of x.
-struct Divisor {
-  uint32_t mul, shift;
-  __device__ __forceinline__ uint32_t quotient(uint32_t x) const { return static_cast<uint32_t>(static_cast<uint64_t>(x) * mul >> shift); }
-};
-Divisor divisor(uint32_t d) {
-  uint32_t l = 0;
-  while ((1ull << l) < d) ++l;
-  return {static_cast<uint32_t>(((1ull << (31 + l)) + d - 1) / d), 31 + l};
-}
-
 struct StoreArgs {
   wk_paged_kv c;
   const uint8_t *src[2];

@@ -295,3 +295,32 @@ def test_an_output_of_a_tensor_subclass(kv):
     O = torch.nn.Parameter(torch.empty_like(Q), requires_grad=False)
     assert PagedKV(kv, K, V).paged_attention(Q, tables, lens, O=O) is O
     assert torch.equal(O, PagedKV(kv, K, V).paged_attention(torch.nn.Parameter(Q, requires_grad=False), tables, lens))
+
+
+def test_tables_with_room_for_more_than_31_bits_of_steps(kv):
+    """3,000 requests whose tables could name 320,000 tokens each, 40 kv heads: more than one launch counts, so there are two."""
+    from paper_2605_22718_b200 import PagedKV
+    n, width = 3000, 20000
+    lens = [(i * 7) % 40 - 1 for i in range(n)]
+    n_pages = sum(-(-max(m, 0) // 16) for m in lens) + 1
+    K, V, _, _ = lib.cache("f16", n_pages, 16, 40, 64)
+    tables = torch.full((n, width), -7, dtype=torch.int32, device="cuda")
+    tables[:, :4] = lib.tables_for(lens, 16, n_pages, 4)
+    dev = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    Q = queries(n, 40, 64, torch.float16)
+    lse = torch.full((n, 40), 77.0, device="cuda")
+    O = torch.full_like(Q, 55)
+    c = PagedKV(kv, K, V)
+    before = kv.launch_count()
+    c.paged_attention(Q, tables, dev, O=O, lse_out=lse)
+    assert kv.launch_count() == before + 2
+    some = torch.tensor([i for i in range(n) if i % 97 == 0 or i > n - 5 or 2676 < i < 2690], device="cuda")
+    keep = some[dev[some] >= 0]
+    ref = lib.attend(Q[keep], K, V, None, None, tables[keep], [lens[i] for i in keep.tolist()])
+    lib.assert_attends(O[keep], lse[keep], ref)
+    assert (O[dev < 0] == 55).all() and (lse[dev < 0] == 77).all() and kv.poll_status() == (0, 0)
+    narrow = tables[:, :4].contiguous()          # the same with room for 64 tokens: one launch, the same rows
+    again, lse2 = torch.full_like(Q, 55), torch.full_like(lse, 77.0)
+    c.paged_attention(Q, narrow, dev, O=again, lse_out=lse2)
+    assert kv.launch_count() == before + 3
+    lib.assert_attends(again[keep], lse2[keep], ref)
