@@ -274,7 +274,7 @@ typedef struct {
   int64_t page_stride;   /* elements, multiples of 16 bytes, the rows of a cache not overlapping */
   int64_t token_stride;
   int64_t head_stride;
-  int32_t n_pages;       /* n_pages * page_tokens < 2^31 */
+  int32_t n_pages;       /* n_pages * page_tokens < 2^31, WK_E4M3: that times n_kv_heads < 2^32 */
   int32_t page_tokens;   /* >= 1 */
   int32_t n_kv_heads;
   int32_t head_dim;      /* 64 or 128 */

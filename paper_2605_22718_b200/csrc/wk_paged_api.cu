@@ -29,7 +29,8 @@ static wk_status check_cache(const wk_paged_kv* c) {
     covered = static_cast<double>(ax[best].stride) * ax[best].n;
     ax[best].n = 1;
   }
-  if (static_cast<int64_t>(c->n_pages) * c->page_tokens > 0x7fffffffLL) return WK_ERR_SHAPE;
+  const int64_t tokens = static_cast<int64_t>(c->n_pages) * c->page_tokens;
+  if (tokens > 0x7fffffffLL || (c->type == WK_E4M3 && tokens * c->n_kv_heads > 0xffffffffLL)) return WK_ERR_SHAPE;
   return WK_OK;
 }
 

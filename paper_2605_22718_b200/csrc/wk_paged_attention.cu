@@ -350,7 +350,7 @@ paged_attention(const __grid_constant__ Params p) {
     int32_t j_up = (of_unit - left) * ST + (lane & (ST - 1));   // this lane's token of the step to look up
     const int32_t* table = p.a.tables + nxt.r * p.a.table_stride;
     int in = 0, out = 0;                     // places in to_come
-    bool whole = left == of_unit;               // the unit at hand began in this run
+    bool whole = left == of_unit;            // the unit at hand began in this run
     bool fresh = true;
     // Where this lane's chunks go: token k * RPI + lane / LPR, swizzled so that eight rows' chunks lie in different banks.
     const uint32_t ring_at = ptx::smem_u32(ring), chunk_l = lane % S::LPR, hi = lane / S::LPR;
@@ -369,8 +369,7 @@ paged_attention(const __grid_constant__ Params p) {
           const bool there = static_cast<uint32_t>(id[k]) < static_cast<uint32_t>(p.a.c.n_pages);
           if (!there && id[k] != -1) bad = WK_DEV_BAD_SLOT;
           row[k] = there ? id[k] * p.page16 + off[k] * p.token16 : kNowhere;
-          // (fewer than 2^30 rows: there are 64 bytes to each, and less than 64 GB)
-          if constexpr (E4) ex[k] = there ? (id[k] * p.a.c.n_kv_heads + kv_ask) * p.a.c.page_tokens + off[k] : 0;
+          if constexpr (E4) ex[k] = there ? (static_cast<uint32_t>(id[k]) * p.a.c.n_kv_heads + kv_ask) * p.a.c.page_tokens + off[k] : 0;
         }
       }
       // ---- step i + STAGES + 1: look up the page ids
@@ -397,7 +396,7 @@ paged_attention(const __grid_constant__ Params p) {
             const uint32_t pos = static_cast<uint32_t>(j >= p.a.sink ? j + nxt.shift : j);
             const uint32_t at = p.by_page.quotient(pos);
             off[k] = pos - at * p.a.c.page_tokens;
-            id[k] = __ldg(table + at);
+            id[k] = table[at];   // (not through the read-only path: the kernel in front may have written it)
           }
         }
       }

@@ -185,3 +185,62 @@ def test_a_context_that_is_not_bound_has_no_status_word(kv):
     torch.cuda.synchronize()
     assert torch.equal(O, want) and kv.poll_status() == (0, 0)
     L.wk_destroy(h)
+
+
+@pytest.mark.parametrize("type_", ["bf16", "e4m3"])
+def test_first_calls_inside_a_capture(type_):
+    """A context's first plan, store and attention may be captured ones."""
+    from paper_2605_22718_b200 import PagedKV, WorldKV
+    fresh = WorldKV(n_layers=1, n_heads=1, tokens_per_frame=8, n_keep=4, pool_slots=1, max_k=1)
+    c = PagedKV.empty(fresh, 20, 16, 4, 128, lib.TYPES[type_])
+    ring, state = c.free_pages()
+    lens, tables = gpu([0, 0]), gpu([[-1] * 10] * 2)
+    x = torch.randn((40, 4, 128), device="cuda").to(torch.bfloat16)
+    Q = torch.randn((2, 12, 128), device="cuda").to(torch.bfloat16)
+    new = gpu([33, 7])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        slots, _ = c.page_plan(lens, new, tables, ring, state, 40)
+        c.page_store(x, x, slots)
+        O = c.paged_attention(Q, tables, lens)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert lens.tolist() == [33, 7] and state.tolist() == [4, 16, 0, 0]
+    ref = lib.attend(Q, c.K, c.V, c.K_exp, c.V_exp, tables, [33, 7])
+    lib.assert_attends(O, ref[1].float(), ref)
+    del graph
+    assert fresh.poll_status() == (0, 0)
+
+
+def test_what_the_kernel_in_front_has_written_is_seen(kv):
+    """Plans, stores and attentions one after the other without a pause, each needing what the one before has just written: the
+    same results as with a wait after every call."""
+    from paper_2605_22718_b200 import PagedKV
+    n, page = 64, 4
+
+    def run(wait):
+        c = PagedKV.empty(kv, 64 * 40, page, 4, 64)
+        ring, state = c.free_pages()
+        lens, tables = gpu([0] * n), torch.full((n, 40), -1, dtype=torch.int32, device="cuda")
+        g = torch.Generator(device="cuda").manual_seed(1)
+        xs = [torch.randn((n * 3, 4, 64), generator=g, device="cuda").to(torch.bfloat16) for _ in range(24)]
+        Q = torch.randn((n, 8, 64), generator=g, device="cuda").to(torch.bfloat16)
+        outs = []
+        three = gpu([3] * n)
+        for x in xs:
+            slots, _ = c.page_plan(lens, three, tables, ring, state, 3 * n)
+            if wait:
+                torch.cuda.synchronize()
+            c.page_store(x, x, slots)
+            if wait:
+                torch.cuda.synchronize()
+            outs.append(c.paged_attention(Q, tables, lens))
+            if wait:
+                torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        return outs
+
+    want = run(True)
+    for _ in range(5):
+        assert all(torch.equal(a, b) for a, b in zip(run(False), want))

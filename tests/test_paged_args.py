@@ -64,6 +64,7 @@ BAD_CACHES = [
     (dict(head_stride=120), ARG), (dict(token_stride=7 * 128), ARG), (dict(page_stride=15 * 8 * 128), ARG),   # rows overlap
     (dict(page_stride=0), ARG), (dict(token_stride=128), ARG),
     (dict(n_pages=1 << 27), SHAPE),                                    # 2^31 slots
+    (dict(E4M3, n_pages=1 << 25, n_kv_heads=8), SHAPE),                # 2^32 exponents
 ]
 GOOD_CACHES = [
     dict(), E4M3, dict(type=binding.WK_F16, head_dim=64), dict(n_pages=1, page_stride=3), dict(page_tokens=1, token_stride=0),
