@@ -271,7 +271,7 @@ typedef struct {
   void* V;               /* the same layout */
   uint8_t* K_exp;        /* WK_E4M3: [n_pages][n_kv_heads][page_tokens], contiguous, 4-byte aligned: a row stands for its */
   uint8_t* V_exp;        /*   codes times 2^(byte - 127), byte in 1 .. 254; otherwise NULL */
-  int64_t page_stride;   /* elements, multiples of 16 bytes, the rows of a cache not overlapping */
+  int64_t page_stride;   /* elements, multiples of 16 bytes, the rows of a cache not overlapping, a head's rows within 64 GB */
   int64_t token_stride;
   int64_t head_stride;
   int32_t n_pages;       /* n_pages * page_tokens < 2^31, WK_E4M3: that times n_kv_heads < 2^32 */
@@ -315,7 +315,7 @@ wk_status wk_page_plan(wk_ctx* ctx, int32_t n_pages, int32_t page_tokens, int32_
  *   WK_E4M3: a row (one token, one head) is stored with the smallest exponent e in -126 .. 127 for which its largest finite
  *             magnitude is at most 448 * 2^e (0 for a row of zeros), each value rounded to the nearest code, ties to even.
  *             Values that are not finite become NaN and set WK_DEV_NONFINITE
- * Errors: WK_ERR_ARG, WK_ERR_SHAPE. */
+ * Errors: WK_ERR_ARG, WK_ERR_SHAPE (2^31 rows of one head or more). */
 wk_status wk_page_store(wk_ctx* ctx, const wk_paged_kv* cache, const void* K_new, const void* V_new, int32_t src_type,
                         int32_t n_tokens, int64_t row_stride, const int32_t* slots, void* stream);
 
@@ -337,8 +337,7 @@ size_t wk_paged_scratch_bytes(const wk_ctx* ctx);
  *             -inf) is O = 0, lse = -inf; a logit that is NaN or +inf makes its row NaN
  *   softmax_scale 0 selects 1/sqrt(head_dim); window 0: all tokens
  *   scratch   wk_paged_scratch_bytes() bytes, 256-byte aligned
- * Errors: WK_ERR_SHAPE (n_heads not a multiple of n_kv_heads, scratch too small, a cache of 64 GB or more),
- * WK_ERR_ARG. */
+ * Errors: WK_ERR_SHAPE (n_heads not a multiple of n_kv_heads, scratch too small), WK_ERR_ARG. */
 wk_status wk_paged_attention(wk_ctx* ctx, const wk_paged_kv* cache, const void* Q, int32_t q_type, int64_t q_stride,
                              int32_t n_req, int32_t n_heads, const int32_t* tables, int32_t max_pages,
                              int64_t table_stride, const int32_t* lens, int32_t window, int32_t sink,

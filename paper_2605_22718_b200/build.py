@@ -60,7 +60,7 @@ def _host_command(source: str, target: str):
     flags = [x for d in includes for x in ("-isystem", d)]
     return ["g++", "-std=c++17", "-O2", "-shared", "-fPIC", "-fvisibility=hidden",
             "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI, *flags, "-o", target, source, "-L", os.path.join(at, "lib"),
-            "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"]
+            "-ltorch_python", "-ltorch_cpu", "-ltorch_cuda", "-lc10", "-lc10_cuda"]
 
 
 def build_all(force: bool = False) -> None:

@@ -6,6 +6,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <ATen/cuda/EmptyTensor.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -70,6 +71,10 @@ bool rows(const at::Tensor* t, int64_t device) {
   return t && on(*t, device) && t->dim() == 3 && t->stride(2) == 1 && (t->size(1) == 1 || t->stride(1) == t->size(2)) &&
          t->size(0) <= std::numeric_limits<int32_t>::max();
 }
+// A contiguous tensor of x's type and device, without the way through the dispatcher.
+at::Tensor empty(at::IntArrayRef sizes, const at::Tensor& x) {
+  return at::Tensor(at::detail::empty_cuda(sizes, x.scalar_type(), x.device(), std::nullopt));
+}
 PyObject* said(const char* what) { return PyUnicode_FromString(what); }
 
 // The library's calls wait where the GPU's queue is full: other Python threads run meanwhile.
@@ -111,8 +116,8 @@ PyObject* page_plan(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
     return said(a.wrong);
   void* stream = a.stream(device);
   if (PyErr_Occurred()) return nullptr;
-  const at::Tensor slots = slots_in ? *slots_in : at::empty({max_tokens}, lens->options());
-  const at::Tensor starts = starts_in ? *starts_in : at::empty({n + 1}, lens->options());
+  const at::Tensor slots = slots_in ? *slots_in : empty({max_tokens}, *lens);
+  const at::Tensor starts = starts_in ? *starts_in : empty({n + 1}, *lens);
   const wk_status st = without_lock([&] { return call_plan(
       ctx, n_pages, page_tokens, static_cast<int32_t>(n), lens->data_ptr<int32_t>(), more->data_ptr<int32_t>(),
       (lens_out ? lens_out : lens)->data_ptr<int32_t>(), tables->data_ptr<int32_t>(), static_cast<int32_t>(tables->size(1)),
@@ -185,7 +190,7 @@ PyObject* paged_attention(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
     return said(a.wrong);
   void* stream = a.stream(device);
   if (PyErr_Occurred()) return nullptr;
-  const at::Tensor O = O_in ? *O_in : at::empty(Q->sizes(), Q->options());
+  const at::Tensor O = O_in ? *O_in : empty(Q->sizes(), *Q);
   if (n > 0) {
     const wk_status st = without_lock([&] { return call_attention(
         ctx, cache, Q->data_ptr(), type_of(Q->scalar_type()), Q->stride(0), static_cast<int32_t>(n), static_cast<int32_t>(heads),

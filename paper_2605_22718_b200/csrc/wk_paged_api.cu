@@ -29,6 +29,10 @@ static wk_status check_cache(const wk_paged_kv* c) {
     covered = static_cast<double>(ax[best].stride) * ax[best].n;
     ax[best].n = 1;
   }
+  // the kernels count places of tokens in 16-byte units of 32 bits, a head's beside them
+  const double most = 4294967295.0 * 16 / (c->type == WK_E4M3 ? 1 : 2);   // elements
+  if (static_cast<double>(c->n_pages - 1) * c->page_stride + static_cast<double>(c->page_tokens - 1) * c->token_stride >= most) return WK_ERR_SHAPE;
+  if (c->n_kv_heads > 1 && c->head_stride >= most) return WK_ERR_SHAPE;
   const int64_t tokens = static_cast<int64_t>(c->n_pages) * c->page_tokens;
   if (tokens > 0x7fffffffLL || (c->type == WK_E4M3 && tokens * c->n_kv_heads > 0xffffffffLL)) return WK_ERR_SHAPE;
   return WK_OK;
@@ -69,6 +73,7 @@ wk_status wk_page_store(wk_ctx* ctx, const wk_paged_kv* cache, const void* K_new
   if (!K_new || !V_new || !slots || !aligned16(K_new) || !aligned16(V_new)) return WK_ERR_ARG;
   if (n_tokens > 1 && (row_stride % 8 || row_stride < static_cast<int64_t>(cache->n_kv_heads) * cache->head_dim))
     return WK_ERR_ARG;
+  if (static_cast<int64_t>(n_tokens) * cache->n_kv_heads > 0x7fffffffLL || row_stride / 8 > 0x7fffffffLL) return WK_ERR_SHAPE;
   WK_USE_DEVICE(ctx);
   return launch_page_store(ctx, *cache, K_new, V_new, src_type, n_tokens, row_stride, slots,
                            static_cast<cudaStream_t>(stream));
@@ -91,11 +96,6 @@ wk_status wk_paged_attention(wk_ctx* ctx, const wk_paged_kv* cache, const void* 
   if (n_req > 1 && table_stride < max_pages) return WK_ERR_ARG;
   if (n_heads % cache->n_kv_heads) return WK_ERR_SHAPE;
   if (scratch_bytes < paged_scratch_bytes(ctx->sm_count)) return WK_ERR_SHAPE;
-  // the kernel counts places in the cache in 16-byte units of 32 bits
-  const int64_t size = cache->type == WK_E4M3 ? 1 : 2;
-  const double reach = (static_cast<double>(cache->n_pages - 1) * cache->page_stride +
-                        static_cast<double>(cache->page_tokens - 1) * cache->token_stride) * size / 16;
-  if (reach >= 4294967295.0) return WK_ERR_SHAPE;
   // positions are 32-bit; a table longer than that cannot be used to its end
   const int64_t room = 0x7fffffffLL / cache->page_tokens;
   WK_USE_DEVICE(ctx);

@@ -131,8 +131,9 @@ page_plan(const __grid_constant__ PlanArgs a) {
   if (lane == 0 && taken) atomicMax(&popped, taken);
   __syncthreads();
 
-  // slots of the new tokens
-  for (int64_t t0 = static_cast<int64_t>(blockIdx.x) * kTokens; t0 < a.max_tokens; t0 += static_cast<int64_t>(gridDim.x) * kTokens) {
+  // slots of the new tokens.  Where there are several blocks, the first has the pages of ended requests to see to instead.
+  const int fillers = max(gridDim.x - 1, 1), filler = gridDim.x > 1 ? static_cast<int>(blockIdx.x) - 1 : 0;
+  for (int64_t t0 = filler < 0 ? a.max_tokens : static_cast<int64_t>(filler) * kTokens; t0 < a.max_tokens; t0 += static_cast<int64_t>(fillers) * kTokens) {
 #pragma unroll
     for (int i = 0; i < kTokens / THREADS; ++i) {
       const int64_t t = t0 + i * THREADS + tid;
@@ -262,60 +263,15 @@ constexpr int kStoreThreads = 128;
 constexpr int kStoreLoads = 4;   // 16-byte loads in flight per thread
 
 struct StoreArgs {
-  wk_paged_kv c;
+  uint8_t *dst[2], *exps[2];
   const uint8_t *src[2];
-  int64_t row_bytes;      // from one source row to the next
-  int32_t n_tokens, rows; // rows per block
+  uint32_t page16, token16, head16, row16;   // strides in units of 16 bytes: of the cache, of the source's rows
+  uint32_t n_rows;                           // rows of K (one token, one head): of V as many
+  int32_t n_pages, page_tokens, n_heads;
   const int32_t* slots;
   uint32_t* status;
   Divisor by_page, by_heads;
 };
-
-// The slot's page and place in it; false: nothing to write.
-__device__ __forceinline__ bool slot_place(const StoreArgs& a, int32_t slot, int64_t* page, int64_t* off) {
-  const uint32_t id = a.by_page.quotient(static_cast<uint32_t>(slot));
-  if (slot < 0 || id >= static_cast<uint32_t>(a.c.n_pages)) {
-    if (slot != -1) report(a.status, WK_DEV_BAD_SLOT);
-    return false;
-  }
-  *page = id;
-  *off = slot - id * a.c.page_tokens;
-  return true;
-}
-
-// Copies rows: bound by memory.  A block takes K or V of a few rows; each thread moves four 16-byte vectors, all loads before the
-// first store.  head_dim is 64 or 128, so a head is 8 or 16 vectors.
-__global__ void __launch_bounds__(kStoreThreads)
-store_rows(const __grid_constant__ StoreArgs a) {
-  dep_release();
-  dep_wait();
-  const int side = blockIdx.y;
-  const int head_shift = a.c.head_dim == 128 ? 4 : 3;
-  const int vecs = a.c.n_kv_heads << head_shift;
-  const int32_t t0 = blockIdx.x * a.rows, n = min(a.rows, a.n_tokens - t0);
-  uint8_t* dst = static_cast<uint8_t*>(side ? a.c.V : a.c.K);
-  const int64_t total = static_cast<int64_t>(n) * vecs;
-  for (int64_t i0 = threadIdx.x; i0 < total; i0 += kStoreLoads * kStoreThreads) {
-    uint4 q[kStoreLoads];
-    uint4* to[kStoreLoads];
-#pragma unroll
-    for (int u = 0; u < kStoreLoads; ++u) {
-      const int64_t i = i0 + u * kStoreThreads;
-      to[u] = nullptr;
-      if (i >= total) continue;
-      const int r = a.rows == 1 ? 0 : static_cast<int>(static_cast<uint32_t>(i) / static_cast<uint32_t>(vecs));
-      const int v = static_cast<int>(i - static_cast<int64_t>(r) * vecs);
-      int64_t page, off;
-      if (!slot_place(a, a.slots[t0 + r], &page, &off)) continue;
-      const int h = v >> head_shift, w = v & ((1 << head_shift) - 1);
-      to[u] = reinterpret_cast<uint4*>(dst + 2 * (page * a.c.page_stride + off * a.c.token_stride + h * a.c.head_stride)) + w;
-      q[u] = __ldcs(reinterpret_cast<const uint4*>(a.src[side] + static_cast<int64_t>(t0 + r) * a.row_bytes) + v);
-    }
-#pragma unroll
-    for (int u = 0; u < kStoreLoads; ++u)
-      if (to[u]) *to[u] = q[u];
-  }
-}
 
 __device__ __forceinline__ void unpack2(uint32_t w, bool bf16, float* lo, float* hi) {
   if (bf16) {
@@ -327,91 +283,107 @@ __device__ __forceinline__ void unpack2(uint32_t w, bool bf16, float* lo, float*
     *hi = f.y;
   }
 }
-// The larger of two magnitudes of 16 bits each: without the sign, both types' bits grow with the magnitude.
-__device__ __forceinline__ uint32_t larger2(uint32_t x, uint32_t y) { return __vmaxu2(x & 0x7fff7fffu, y & 0x7fff7fffu); }
+// The larger of two magnitudes of 16 bits each (no signs): both types' bits grow with the magnitude.
+__device__ __forceinline__ uint32_t larger2(uint32_t x, uint32_t y) { return __vmaxs2(x, y); }
 
-// Rows in 8 bits: a row (one token, one head) belongs to head_dim / 8 neighbouring lanes, 16 bytes each.  The exponent is read off
-// the bits of the largest magnitude: amax = m * 2^x with 1 <= m < 2 fits 448 * 2^e = 1.75 * 2^(e + 8) for e = x - 8 if m <= 1.75,
-// else for x - 7.  A power of two keeps the scaling exact (the one rounding is that to the code) and costs a byte per row; codes of
-// 17 binades leave no accuracy to be won from a finer scale.  The largest magnitude is found on the 16-bit patterns; a row in
-// which that is Inf or NaN looks again among its finite values.
-template <bool BF16, int D>
-__global__ void __launch_bounds__(kStoreThreads)
-store_rows_e4m3(const __grid_constant__ StoreArgs a) {
-  constexpr int LANES = D / 8, ROWS = kStoreThreads / LANES;   // lanes per row, rows at a time
+// Eight values of a row, which belongs to LANES neighbouring lanes, in 8 bits; *byte: the row's exponent + 127.  The exponent is read
+// off the bits of the row's largest magnitude: amax = m * 2^x with 1 <= m < 2 fits 448 * 2^e = 1.75 * 2^(e + 8) for e = x - 8 if
+// m <= 1.75, else for x - 7.  A power of two keeps the scaling exact (the one rounding is that to the code) and costs a byte per
+// row; codes of 17 binades leave no accuracy to be won from a finer scale.  The largest magnitude is found on the 16-bit patterns;
+// a row in which that is Inf or NaN looks again among its finite values.
+template <bool BF16, int LANES>
+__device__ __forceinline__ uint2 to_codes(uint4 q, int* byte, bool* odd) {
   constexpr uint32_t kInf = BF16 ? 0x7f80u : 0x7c00u;
-  dep_release();
-  dep_wait();
-  const int side = blockIdx.y, l = threadIdx.x % LANES;
-  uint8_t* dst = static_cast<uint8_t*>(side ? a.c.V : a.c.K);
-  uint8_t* exps = side ? a.c.V_exp : a.c.K_exp;
-  const int32_t t0 = blockIdx.x * a.rows, n = min(a.rows, a.n_tokens - t0) * a.c.n_kv_heads;   // this block's rows
-#pragma unroll 1
-  for (int32_t k = 0; k < n; k += kStoreLoads * ROWS) {   // the same number for all lanes: they exchange values
-    uint4 q[kStoreLoads];
-    int32_t slot[kStoreLoads], head[kStoreLoads];
+  const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+  uint32_t m = larger2(larger2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu), larger2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
 #pragma unroll
-    for (int u = 0; u < kStoreLoads; ++u) {
-      const int32_t i = k + u * ROWS + threadIdx.x / LANES;
-      q[u] = make_uint4(0, 0, 0, 0);
-      slot[u] = -1;
-      head[u] = 0;
-      if (i < n) {
-        const int32_t t = a.by_heads.quotient(i);
-        head[u] = i - t * a.c.n_kv_heads;
-        slot[u] = a.slots[t0 + t];
-        q[u] = __ldcs(reinterpret_cast<const uint4*>(a.src[side] + static_cast<int64_t>(t0 + t) * a.row_bytes) + head[u] * LANES + l);
-      }
+  for (int d = 1; d < LANES; d <<= 1) m = larger2(m, __shfl_xor_sync(0xffffffffu, m, d));
+  uint32_t top16 = max(m & 0xffffu, m >> 16);
+  *odd = top16 >= kInf;
+  if (__any_sync(0xffffffffu, *odd)) {
+    uint32_t fine = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t lo = w[j] & 0x7fffu, hi = w[j] >> 16 & 0x7fffu;
+      fine = max(fine, max(lo < kInf ? lo : 0u, hi < kInf ? hi : 0u));
     }
 #pragma unroll
-    for (int u = 0; u < kStoreLoads; ++u) {
-      const uint32_t w[4] = {q[u].x, q[u].y, q[u].z, q[u].w};
-      uint32_t m = larger2(larger2(w[0], w[1]), larger2(w[2], w[3]));
+    for (int d = 1; d < LANES; d <<= 1) fine = max(fine, __shfl_xor_sync(0xffffffffu, fine, d));
+    if (*odd) top16 = fine;
+  }
+  // a bf16 below the normal numbers reads x = -127 here and ends at the least exponent, as it should
+  const uint32_t bits = BF16 ? top16 << 16 : __float_as_uint(__half2float(__ushort_as_half(static_cast<uint16_t>(top16))));
+  *byte = top16 == 0 ? 127 : max(1, static_cast<int>((bits + 0x1fffffu) >> 23) - 8);   // (a mantissa above 0.75 carries)
+  const float scale = __uint_as_float(static_cast<uint32_t>(254 - *byte) << 23);          // 2^-e; byte is at most 247
+  float x[8];
 #pragma unroll
-      for (int d = 1; d < LANES; d <<= 1) m = __vmaxu2(m, __shfl_xor_sync(0xffffffffu, m, d));
-      uint32_t top16 = max(m & 0xffffu, m >> 16);
-      const bool odd = top16 >= kInf;
-      if (__any_sync(0xffffffffu, odd)) {
-        uint32_t fine = 0;
+  for (int j = 0; j < 4; ++j) {
+    unpack2(w[j], BF16, &x[2 * j], &x[2 * j + 1]);
+    x[2 * j] *= scale;
+    x[2 * j + 1] *= scale;
+  }
+  if (*odd) {   // infinities, too, become NaN; the conversion would make them the largest code
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t lo = w[j] & 0x7fffu, hi = w[j] >> 16 & 0x7fffu;
-          fine = max(fine, max(lo < kInf ? lo : 0u, hi < kInf ? hi : 0u));
-        }
+    for (int j = 0; j < 8; ++j)
+      if (!(fabsf(x[j]) <= 3.402823466e38f)) x[j] = __int_as_float(0x7fffffff);
+  }
+  uint32_t code[2];
 #pragma unroll
-        for (int d = 1; d < LANES; d <<= 1) fine = max(fine, __shfl_xor_sync(0xffffffffu, fine, d));
-        if (odd) top16 = fine;
+  for (int j = 0; j < 2; ++j)
+    asm("{\n\t.reg .b16 l, h;\n\tcvt.rn.satfinite.e4m3x2.f32 l, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 h, %4, %3;\n\tmov.b32 %0, {l, h};\n\t}"
+        : "=r"(code[j]) : "f"(x[4 * j]), "f"(x[4 * j + 1]), "f"(x[4 * j + 2]), "f"(x[4 * j + 3]));
+  return make_uint2(code[0], code[1]);
+}
+
+// SRC: the type of the source where the cache is in 8 bits, -1 where rows are copied.  A row belongs to D / 8 neighbouring lanes,
+// 16 bytes each; a thread has four rows, whose loads are all under way before the first is worked on.  Strides and divisions in 32
+// bits matter: with 64 the copies filled 68 % of the issue slots and the rows in 8 bits 79 %.  8,937 tokens of 12 heads (110 MB): 19.5
+// us -> 18.3 = 6.0 TB/s; 40,001 tokens of 8 heads to 8 bits (247 MB): 52.9 -> 45.5 = 5.4 TB/s, the scattered exponent bytes 5 of them.
+template <int SRC, int D>
+__global__ void __launch_bounds__(kStoreThreads)
+store_rows(const __grid_constant__ StoreArgs a) {
+  constexpr int LANES = D / 8, ROWS = kStoreThreads / LANES;
+  dep_release();
+  dep_wait();
+  const int side = blockIdx.y;
+  const uint32_t l = threadIdx.x % LANES;
+  uint4 q[kStoreLoads];
+  int32_t slot[kStoreLoads];
+  uint32_t head[kStoreLoads];
+#pragma unroll
+  for (int u = 0; u < kStoreLoads; ++u) {
+    const uint32_t i = (blockIdx.x * kStoreLoads + u) * ROWS + threadIdx.x / LANES;
+    q[u] = make_uint4(0, 0, 0, 0);
+    slot[u] = -1;
+    head[u] = 0;
+    if (i < a.n_rows) {
+      const uint32_t t = a.by_heads.quotient(i);
+      head[u] = i - t * a.n_heads;
+      slot[u] = a.slots[t];
+      q[u] = __ldcs(reinterpret_cast<const uint4*>(a.src[side]) + static_cast<uint64_t>(t) * a.row16 + (head[u] * LANES + l));
+    }
+  }
+#pragma unroll
+  for (int u = 0; u < kStoreLoads; ++u) {
+    int byte = 0;
+    bool odd = false;
+    uint2 code;
+    if constexpr (SRC >= 0) code = to_codes<SRC == WK_BF16, LANES>(q[u], &byte, &odd);   // (all lanes: they exchange values)
+    const uint32_t id = a.by_page.quotient(static_cast<uint32_t>(slot[u]));
+    if (slot[u] < 0 || id >= static_cast<uint32_t>(a.n_pages)) {
+      if (slot[u] != -1) report(a.status, WK_DEV_BAD_SLOT);
+      continue;
+    }
+    const uint32_t off = slot[u] - id * a.page_tokens;
+    uint4* const row = reinterpret_cast<uint4*>(a.dst[side]) + (static_cast<uint64_t>(head[u]) * a.head16 + (id * a.page16 + off * a.token16));
+    if constexpr (SRC < 0) {
+      row[l] = q[u];
+    } else {
+      reinterpret_cast<uint2*>(row)[l] = code;
+      if (l == 0) {
+        a.exps[side][(id * a.n_heads + head[u]) * a.page_tokens + off] = static_cast<uint8_t>(byte);
+        if (odd) report(a.status, WK_DEV_NONFINITE);
       }
-      // byte = e + 127; a bf16 below the normal numbers reads x = -127 here and ends at the least exponent, as it should
-      const uint32_t bits = BF16 ? top16 << 16 : __float_as_uint(__half2float(__ushort_as_half(static_cast<uint16_t>(top16))));
-      const int byte = top16 == 0 ? 127 : max(1, static_cast<int>(bits >> 23) - 8 + ((bits & 0x7fffffu) > 0x600000u ? 1 : 0));
-      int64_t page, off;
-      if (!slot_place(a, slot[u], &page, &off)) continue;
-      const float scale = __uint_as_float(static_cast<uint32_t>(254 - byte) << 23);   // 2^-e; byte is at most 247
-      float x[8];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        unpack2(w[j], BF16, &x[2 * j], &x[2 * j + 1]);
-        x[2 * j] *= scale;
-        x[2 * j + 1] *= scale;
-      }
-      if (odd) {   // infinities, too, become NaN; the conversion would make them the largest code
-        if (l == 0) report(a.status, WK_DEV_NONFINITE);
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-          if (!(fabsf(x[j]) <= 3.402823466e38f)) x[j] = __int_as_float(0x7fffffff);
-      }
-      uint32_t code[2];
-#pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        uint16_t lo, hi;
-        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(x[4 * j + 1]), "f"(x[4 * j]));
-        asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(x[4 * j + 3]), "f"(x[4 * j + 2]));
-        code[j] = lo | static_cast<uint32_t>(hi) << 16;
-      }
-      *reinterpret_cast<uint2*>(dst + page * a.c.page_stride + off * a.c.token_stride + head[u] * a.c.head_stride + 8 * l) =
-          make_uint2(code[0], code[1]);
-      if (l == 0) exps[(page * a.c.n_kv_heads + head[u]) * a.c.page_tokens + off] = static_cast<uint8_t>(byte);
     }
   }
 }
@@ -423,7 +395,7 @@ wk_status launch_page_plan(wk_ctx* ctx, const PlanArgs& a, cudaStream_t s) {
   // without new tokens); four new tokens per thread.
   const auto blocks = [&](int64_t threads) {
     const int64_t n = (static_cast<int64_t>(a.max_tokens) + 4 * threads - 1) / (4 * threads);
-    return static_cast<int>(n < 1 ? 1 : n < ctx->sm_count ? n : ctx->sm_count);
+    return static_cast<int>(n <= 1 ? 1 : n + 1 < ctx->sm_count ? n + 1 : ctx->sm_count);
   };
   if (a.n_req <= kPlanPer * 256) launch_chained(page_plan<256>, dim3(blocks(256)), dim3(256), 0, s, a);
   else launch_chained(page_plan<1024>, dim3(blocks(1024)), dim3(1024), 0, s, a);
@@ -432,25 +404,32 @@ wk_status launch_page_plan(wk_ctx* ctx, const PlanArgs& a, cudaStream_t s) {
 
 wk_status launch_page_store(wk_ctx* ctx, const wk_paged_kv& c, const void* K_new, const void* V_new, int src_type, int n_tokens,
                             int64_t row_stride, const int32_t* slots, cudaStream_t s) {
+  const int es = c.type == WK_E4M3 ? 1 : 2;
   StoreArgs a;
-  a.c = c;
+  a.dst[0] = static_cast<uint8_t*>(c.K);
+  a.dst[1] = static_cast<uint8_t*>(c.V);
+  a.exps[0] = c.K_exp;
+  a.exps[1] = c.V_exp;
   a.src[0] = static_cast<const uint8_t*>(K_new);
   a.src[1] = static_cast<const uint8_t*>(V_new);
-  a.row_bytes = row_stride * 2;
-  a.n_tokens = n_tokens;
+  a.page16 = static_cast<uint32_t>(c.page_stride * es / 16);
+  a.token16 = static_cast<uint32_t>(c.token_stride * es / 16);
+  a.head16 = static_cast<uint32_t>(c.head_stride * es / 16);
+  a.row16 = static_cast<uint32_t>(row_stride * 2 / 16);
+  a.n_rows = static_cast<uint32_t>(n_tokens) * c.n_kv_heads;
+  a.n_pages = c.n_pages;
+  a.page_tokens = c.page_tokens;
+  a.n_heads = c.n_kv_heads;
   a.slots = slots;
   a.status = ctx->bound ? ctx->status_dev : nullptr;
   a.by_page = divisor(c.page_tokens);
   a.by_heads = divisor(c.n_kv_heads);
-  const int64_t vecs = static_cast<int64_t>(c.n_kv_heads) * c.head_dim / 8;
-  const int64_t rows = kStoreLoads * kStoreThreads / vecs;
-  a.rows = rows > 1 ? static_cast<int>(rows) : 1;
-  const dim3 grid(static_cast<unsigned>((n_tokens + a.rows - 1) / a.rows), 2);
   const bool wide = c.head_dim == 128;
-  void (*kernel)(const StoreArgs) = store_rows;
-  if (c.type == WK_E4M3 && src_type == WK_BF16) kernel = wide ? store_rows_e4m3<true, 128> : store_rows_e4m3<true, 64>;
-  else if (c.type == WK_E4M3) kernel = wide ? store_rows_e4m3<false, 128> : store_rows_e4m3<false, 64>;
-  launch_chained(kernel, grid, dim3(kStoreThreads), 0, s, a);
+  const uint32_t rows = kStoreThreads / (c.head_dim / 8) * kStoreLoads;
+  void (*kernel)(const StoreArgs) = wide ? store_rows<-1, 128> : store_rows<-1, 64>;
+  if (c.type == WK_E4M3 && src_type == WK_BF16) kernel = wide ? store_rows<WK_BF16, 128> : store_rows<WK_BF16, 64>;
+  else if (c.type == WK_E4M3) kernel = wide ? store_rows<WK_F16, 128> : store_rows<WK_F16, 64>;
+  launch_chained(kernel, dim3((a.n_rows - 1) / rows + 1, 2), dim3(kStoreThreads), 0, s, a);
   return after_launch(ctx);
 }
 
