@@ -1,6 +1,6 @@
 // Argument marshalling of the token-level cache's calls (include/wk.h) for PyTorch tensors: checks, output allocation, the call.  These
 // are made once per layer and token, and the kernels behind them take 2 to 20 us for small batches: marshalled in Python an
-// attention call costs the host 9.6 us, a plan 11, a store 5.9; here 4.0, 5.5, 2.9.
+// attention call costs the host 9.6 us, a plan 11, a store 5.9; here 4.0, 5.0, 2.9.
 //
 // Each function returns its tensors; a str that says what is wrong with an argument; or the status of a call that failed, as an int.
 #include <Python.h>

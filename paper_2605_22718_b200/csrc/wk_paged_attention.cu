@@ -490,18 +490,24 @@ paged_attention(const __grid_constant__ Params p) {
         float top[NT][2], topw[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) top[nt][0] = top[nt][1] = topw[nt][0] = topw[nt][1] = -INFINITY;
-        float vpower[E4 ? ST / 16 : 1][2];
+        float vpower[E4 ? ST / 16 : 1][2], k_of[S::RL], v_of[S::RL];
+        if constexpr (E4) {   // a lane for each token: its key's power of two, its value's exponent
+#pragma unroll
+          for (int k = 0; k < S::RL; ++k) {
+            const uint2 w2 = *reinterpret_cast<const uint2*>(exps + slot * S::META + 8 * ((lane & (ST - 1)) + 32 * k));
+            const uint32_t byte = (masks[warp][slot][S::RL + 2 * k] >> lane & 1) * 8 + (masks[warp][slot][S::RL + 2 * k + 1] >> lane & 1) * 16;
+            k_of[k] = __uint_as_float((w2.x >> byte & 255u) << 23);
+            v_of[k] = static_cast<float>(static_cast<int>(w2.y >> byte & 255u) - 127);
+          }
+        }
 #pragma unroll
         for (int t = 0; t < ST / 16; ++t)
 #pragma unroll
           for (int hh = 0; hh < 2; ++hh) {
             float kscale = 1.f;
             if constexpr (E4) {
-              const int at = t % 2 * 16 + hh * 8 + g;
-              const uint2 w2 = *reinterpret_cast<const uint2*>(exps + slot * S::META + 8 * (t * 16 + hh * 8 + g));
-              const uint32_t byte = (masks[warp][slot][S::RL + t / 2 * 2] >> at & 1) | (masks[warp][slot][S::RL + t / 2 * 2 + 1] >> at & 1) << 1;
-              kscale = __uint_as_float((w2.x >> (8 * byte) & 255u) << 23);
-              vpower[t][hh] = static_cast<float>(static_cast<int>(w2.y >> (8 * byte) & 255u) - 127);
+              kscale = __shfl_sync(0xffffffffu, k_of[t / 2 % S::RL], t % 2 * 16 + hh * 8 + g);
+              vpower[t][hh] = __shfl_sync(0xffffffffu, v_of[t / 2 % S::RL], t % 2 * 16 + hh * 8 + g);
             }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
@@ -572,6 +578,14 @@ paged_attention(const __grid_constant__ Params p) {
         // ---- weights, and O^T += V^T P^T
         const int r8 = lane & 7, sw = ROW == 64 ? r8 >> 1 : r8;
         const uint32_t at = v_at + ((lane >> 4) * 8 + r8) * ROW + (((lane >> 3 & 1) ^ sw) << 4);
+        float at_sum[NT][2], at_w[NT][2];   // the references, 0 where no key has had weight
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            at_sum[nt][e] = ref[nt][e] == -INFINITY ? 0.f : ref[nt][e];
+            at_w[nt][e] = refw[nt][e] == -INFINITY ? 0.f : refw[nt][e];
+          }
 #pragma unroll
         for (int t = 0; t < ST / 16; ++t) {
           uint32_t pf[NT][2];
@@ -580,9 +594,9 @@ paged_attention(const __grid_constant__ Params p) {
             float q[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-              q[e] = ex2_approx(s[t][nt][e] - (ref[nt][e & 1] == -INFINITY ? 0.f : ref[nt][e & 1]));
+              q[e] = ex2_approx(s[t][nt][e] - at_sum[nt][e & 1]);
               sum[nt][e & 1] += q[e];
-              if constexpr (E4) q[e] = ex2_approx(w[t][nt][e] - (refw[nt][e & 1] == -INFINITY ? 0.f : refw[nt][e & 1]));
+              if constexpr (E4) q[e] = ex2_approx(w[t][nt][e] - at_w[nt][e & 1]);
             }
             pf[nt][0] = transpose8x8(pack2<BF>(q[0], q[1]));
             pf[nt][1] = transpose8x8(pack2<BF>(q[2], q[3]));
