@@ -19,6 +19,8 @@
 //   * Softmax.  Per query head a reference close to the running maximum: it moves only when a logit exceeds it by more than 8 (in
 //     log2), which one vote per step finds out, so weights reach at most 2^8; sums are fp32.  Weights are rounded to the type of V
 //     for the second product (bf16 or fp16, half a step 2^-8 or 2^-11 of the weight; the normalising sum is of the unrounded ones).
+//     fp16 has steps of 2^-24 at its lower end, and a long tail of small weights may add up to all that a row has: there the
+//     weights are taken 2^7 times as large (at most 2^15), so that one is off by 2^-32 of the largest at most.
 //   * 8 bits.  Codes are exact in fp16.  A key's power of two joins the logit's scale, a value's is added to the logit that its
 //     weight is taken from (with a reference of its own), so that both products have fp16 operands of ordinary size; Q is brought
 //     into fp16 by a power of two per row, exactly.
@@ -35,7 +37,8 @@ namespace wk {
 namespace {
 
 constexpr uint32_t kNowhere = 0xffffffffu;   // row offset of a token that is not attended
-constexpr float kLazy = 8.f;                 // how far (log2) a logit may exceed the reference
+constexpr float kLazy = 8.f;                 // how far (log2) a logit may exceed the largest that the reference was taken from
+constexpr float kUp = 7.f;                   // how far (log2) below that the reference of weights in fp16 lies
 constexpr float kLn2 = 0.6931471805599453f, kLog2e = 1.4426950408889634f;
 constexpr int kShortRun = 4, kWhole = 8;     // where runs are that short, CTAs go round units of up to so many steps
 constexpr int kLongRun = 24;                 // steps per warp from which on heads are walked side by side
@@ -256,6 +259,7 @@ paged_attention(const __grid_constant__ Params p) {
   constexpr int ST = S::ST, PADDED = S::PADDED, ROW = S::ROW, W = S::W, THREADS = 32 * W, STAGES = S::STAGES;
   constexpr bool E4 = MODE == WK_E4M3, BF = MODE == WK_BF16;
   constexpr int MT = D / 16;   // row tiles of O^T, and steps along the dimensions in S
+  constexpr float UP = MODE == WK_F16 ? kUp : 0.f;   // (in 8 bits the sum has a reference of its own, and the weights' lies kUp below)
   extern __shared__ __align__(1024) uint8_t dyn[];
   __shared__ uint32_t pre[THREADS], parts[W];
   __shared__ float plse[2 * W][8 * NT];
@@ -548,23 +552,26 @@ paged_attention(const __grid_constant__ Params p) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int e = 0; e < 2; ++e) moved |= top[nt][e] > ref[nt][e] + kLazy || (E4 && topw[nt][e] > refw[nt][e] + kLazy);
+          for (int e = 0; e < 2; ++e)   // (differences: they are exact where it matters, so no weight passes 2^15, however large logits are)
+            moved |= top[nt][e] - ref[nt][e] > UP + kLazy || (E4 && topw[nt][e] - refw[nt][e] > kUp + kLazy);
         if (__any_sync(0xffffffffu, moved)) {
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-              float m = fmaxf(top[nt][e], ref[nt][e]), mw = fmaxf(topw[nt][e], refw[nt][e]);
+              float m = fmaxf(top[nt][e], ref[nt][e] + UP), mw = fmaxf(topw[nt][e], refw[nt][e] + kUp);
 #pragma unroll
               for (int d = 4; d < 32; d <<= 1) {
                 m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, d));
                 if (E4) mw = fmaxf(mw, __shfl_xor_sync(0xffffffffu, mw, d));
               }
+              m -= UP;
               const float f = m == -INFINITY ? 1.f : ex2_approx(ref[nt][e] - m);
               sum[nt][e] *= f;
               ref[nt][e] = m;
               float fw = f;
               if (E4) {
+                mw -= kUp;
                 fw = mw == -INFINITY ? 1.f : ex2_approx(refw[nt][e] - mw);
                 refw[nt][e] = mw;
               }
@@ -682,7 +689,8 @@ paged_attention(const __grid_constant__ Params p) {
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) l += __shfl_xor_sync(0xffffffffu, l, d);
             sum[nt][e] = l == 0.f ? -INFINITY : ref[nt][e] + __log2f(l);   // log-sum-exp (log2)
-            f[nt][e] = l == 0.f ? 0.f : __fdividef(E4 ? ex2_approx(refw[nt][e] - ref[nt][e]) : 1.f, l);
+            // (8 bits: the power in two parts, for values up to bf16's largest)
+            f[nt][e] = l == 0.f ? 0.f : E4 ? __fdividef(ex2_approx(refw[nt][e] - ref[nt][e] + 4.f), 16.f * l) : __fdividef(1.f, l);
           }
       }
       if (i + 1 < steps) {   // Q of the unit that comes next: row g of every tile
