@@ -555,6 +555,39 @@ paged_attention(const __grid_constant__ Params p) {
           for (int e = 0; e < 2; ++e)   // (differences: they are exact where it matters, so no weight passes 2^15, however large logits are)
             moved |= top[nt][e] - ref[nt][e] > UP + kLazy || (E4 && topw[nt][e] - refw[nt][e] > kUp + kLazy);
         if (__any_sync(0xffffffffu, moved)) {
+          if constexpr (E4) {
+            // A row of zeros is stored with power 1, which may lie far above the other rows', and would take the weights' reference
+            // along: it gets no weight.  (Below the reference it does no harm, so that rows are looked at here only.)
+            bool none = false;
+#pragma unroll
+            for (int k = 0; k < S::RL; ++k) {
+              if (!__any_sync(0xffffffffu, v_of[k] == 0.f)) continue;
+              const uint4* const x = reinterpret_cast<const uint4*>(ring + slot * S::STEP + S::STEP / 2 + ((lane & (ST - 1)) + 32 * k) * ROW);
+              uint32_t bits = 0;
+#pragma unroll 1
+              for (int j = 0; j < ROW / 16; ++j) bits |= x[j].x | x[j].y | x[j].z | x[j].w;   // (all of the row, in whichever order)
+              const uint32_t zero = __ballot_sync(0xffffffffu, v_of[k] == 0.f && !(bits & 0x7f7f7f7fu));
+              none |= zero != 0;
+#pragma unroll
+              for (int t = 2 * k; t < 2 * k + 2; ++t)
+#pragma unroll
+                for (int hh = 0; hh < 2; ++hh)
+                  if (zero >> (t % 2 * 16 + hh * 8 + g) & 1) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) w[t][nt][2 * hh] = w[t][nt][2 * hh + 1] = -INFINITY;
+                  }
+            }
+            if (none) {
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                  topw[nt][e] = -INFINITY;
+#pragma unroll
+                  for (int t = 0; t < ST / 16; ++t) topw[nt][e] = fmaxf(topw[nt][e], fmaxf(w[t][nt][e], w[t][nt][2 + e]));
+                }
+            }
+          }
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt)
 #pragma unroll

@@ -107,3 +107,47 @@ def test_values_of_any_size_in_8_bits(kv, size):
     # weights off by half a step of fp16, exponentials and sums of 100 values by 2^-15 together, the output by half a step of bf16
     assert ((O - want).abs() <= (2.0 ** -8 + 2.0 ** -11 + 2.0 ** -14) * want).all(), (O / want).max().item()
     assert kv.poll_status() == (0, 0)
+
+
+@pytest.mark.parametrize("size", [2.0 ** -40, 2.0 ** -20, 2.0 ** -14, 1.0, 300.0])
+@pytest.mark.parametrize("d,page,n", [(64, 16, 100), (128, 16, 333), (128, 5, 33)])
+@pytest.mark.parametrize("signed", [False, True])
+def test_rows_of_zeros_beside_small_values_in_8_bits(kv, size, d, page, n, signed):
+    """A row of zeros is stored with the power 1: it lies far above the power of small values, and has nothing to add to them."""
+    from paper_2605_22718_b200 import PagedKV
+    n_pages = -(-n // page)
+    c = PagedKV.empty(kv, n_pages, page, 2, d, torch.float8_e4m3fn)
+    g = torch.Generator(device="cuda").manual_seed(n)
+    K = torch.randn((n, 2, d), generator=g, device="cuda").to(torch.bfloat16)
+    V = (size * (1 + torch.rand((n, 2, d), generator=g, device="cuda"))).to(torch.bfloat16)
+    V[::7, 0] = 0
+    V[n - 1, 1] = 0
+    if signed:
+        V *= torch.where(torch.arange(n, device="cuda") % 2 == 0, 1, -1)[:, None, None]     # zeros of either sign
+        V[..., 0] = V[..., 0].abs()
+    c.page_store(K, V, torch.arange(n, dtype=torch.int32, device="cuda"))
+    if n > 30:
+        V[28, 1] = 0                                            # zeros under another power: a cache that is written otherwise
+        c.V.view(-1, 2, d).view(torch.uint8)[28, 1] = 0
+    Q = torch.randn((1, 8, d), generator=g, device="cuda").to(torch.float16)
+    tables = torch.arange(n_pages, dtype=torch.int32, device="cuda")[None]
+    lens = torch.tensor([n], dtype=torch.int32, device="cuda")
+    O = c.paged_attention(Q.to(torch.bfloat16), tables, lens).double()
+    assert torch.equal((c.V_exp.transpose(1, 2).reshape(-1, 2)[:n] == 127)[::7, 0], torch.ones((n + 6) // 7, dtype=torch.bool, device="cuda"))
+    rows = lambda x, e: x.reshape(-1, 2, d)[:n].double() * torch.pow(2.0, e.transpose(1, 2).reshape(-1, 2)[:n].double() - 127)[..., None]  # noqa: E731
+    k, v = rows(c.K, c.K_exp), rows(c.V, c.V_exp)
+    q = Q.to(torch.bfloat16).double().view(2, 4, d)
+    logits = torch.einsum("hgd,nhd->hgn", q, k) / d ** 0.5
+    p = torch.softmax(logits, -1)
+    want = torch.einsum("hgn,nhd->hgd", p, v).reshape(1, 8, d)
+    mags = torch.einsum("hgd,nhd->hgn", q.abs(), k.abs()).amax() / d ** 0.5
+    # per weight: half a step of fp16, what a logit is off by (d products in 32 bits), the exponential; sums of n values; bf16
+    rel = 2.0 ** -11 + 2 * ((d + 4) * 2.0 ** -23 * mags + 2.0 ** -22 * logits.abs().amax()) + 2.0 ** -22 + 2 * (n + 16) * 2.0 ** -23
+    heavy = torch.einsum("hgn,nhd->hgd", p, v.abs()).reshape(1, 8, d)
+    # weights (times their row's power) below 2^-14 of 2^7 times the largest: off by 2^-32 of that, times codes of up to 448
+    ve = torch.where(v.abs().amax(-1) > 0, torch.pow(2.0, c.V_exp.transpose(1, 2).reshape(-1, 2)[:n].double() - 127), 0.0)
+    low = n * 2.0 ** -32 * 448 * (p * ve.t()[:, None]).amax(-1).reshape(1, 8, 1)
+    tol = rel * heavy + low
+    tol = tol + 2.0 ** -8 * (want.abs() + tol)
+    assert ((O - want).abs() <= tol).all(), ((O - want).abs() / tol).max().item()
+    assert kv.poll_status() == (0, 0)
