@@ -367,6 +367,9 @@ class PagedKV:
     strides that are multiples of 16 bytes (last axis contiguous; K and V alike).  In 8 bits K_exp and V_exp are uint8
     [n_pages, n_kv_heads, page_tokens], contiguous.  ``PagedKV.empty`` allocates them.  A cache made from n_pages and
     page_tokens alone only plans.  Method names and arguments mirror include/wk.h.
+
+    A call runs on ``stream``, or on the current one.  What it allocates (slots, starts, O) belongs to that stream, as with
+    ``torch.cuda.stream``: to use it on another stream, let that wait, and ``record_stream`` it there.
     """
 
     def __init__(self, kv: WorldKV, K: Optional[torch.Tensor] = None, V: Optional[torch.Tensor] = None,

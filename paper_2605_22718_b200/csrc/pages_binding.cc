@@ -7,11 +7,14 @@
 
 #include <ATen/ATen.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDAGuard.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <limits>
+#include <optional>
 
 #include "../../include/wk.h"
 
@@ -54,8 +57,10 @@ struct Arguments {
   void* stream(int64_t device) {
     PyObject* o = args[at++];
     if (o == Py_None) return c10::cuda::getCurrentCUDAStream(static_cast<c10::DeviceIndex>(device)).stream();
-    return PyLong_AsVoidPtr(o);
+    given = c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(PyLong_AsVoidPtr(o)), static_cast<c10::DeviceIndex>(device));
+    return given->stream();
   }
+  std::optional<c10::cuda::CUDAStream> given;   // the caller's stream, if it is not left to be the current one
 };
 
 bool on(const at::Tensor& t, int64_t device) { return t.is_cuda() && t.get_device() == device; }
@@ -71,8 +76,11 @@ bool rows(const at::Tensor* t, int64_t device) {
   return t && on(*t, device) && t->dim() == 3 && t->stride(2) == 1 && (t->size(1) == 1 || t->stride(1) == t->size(2)) &&
          t->size(0) <= std::numeric_limits<int32_t>::max();
 }
-// A contiguous tensor of x's type and device, without the way through the dispatcher.
-at::Tensor empty(at::IntArrayRef sizes, const at::Tensor& x) {
+// A contiguous tensor of x's type and device, without the way through the dispatcher.  It belongs to the stream that the call runs
+// on, as if that were the current one: its memory was used on that stream only, and is used on that stream next.
+at::Tensor empty(at::IntArrayRef sizes, const at::Tensor& x, const Arguments& a) {
+  c10::cuda::OptionalCUDAStreamGuard guard;
+  if (a.given) guard.reset_stream(*a.given);
   return at::Tensor(at::detail::empty_cuda(sizes, x.scalar_type(), x.device(), std::nullopt));
 }
 PyObject* said(const char* what) { return PyUnicode_FromString(what); }
@@ -116,8 +124,8 @@ PyObject* page_plan(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
     return said(a.wrong);
   void* stream = a.stream(device);
   if (PyErr_Occurred()) return nullptr;
-  const at::Tensor slots = slots_in ? *slots_in : empty({max_tokens}, *lens);
-  const at::Tensor starts = starts_in ? *starts_in : empty({n + 1}, *lens);
+  const at::Tensor slots = slots_in ? *slots_in : empty({max_tokens}, *lens, a);
+  const at::Tensor starts = starts_in ? *starts_in : empty({n + 1}, *lens, a);
   const wk_status st = without_lock([&] { return call_plan(
       ctx, n_pages, page_tokens, static_cast<int32_t>(n), lens->data_ptr<int32_t>(), more->data_ptr<int32_t>(),
       (lens_out ? lens_out : lens)->data_ptr<int32_t>(), tables->data_ptr<int32_t>(), static_cast<int32_t>(tables->size(1)),
@@ -190,7 +198,7 @@ PyObject* paged_attention(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
     return said(a.wrong);
   void* stream = a.stream(device);
   if (PyErr_Occurred()) return nullptr;
-  const at::Tensor O = O_in ? *O_in : empty(Q->sizes(), *Q);
+  const at::Tensor O = O_in ? *O_in : empty(Q->sizes(), *Q, a);
   if (n > 0) {
     const wk_status st = without_lock([&] { return call_attention(
         ctx, cache, Q->data_ptr(), type_of(Q->scalar_type()), Q->stride(0), static_cast<int32_t>(n), static_cast<int32_t>(heads),
