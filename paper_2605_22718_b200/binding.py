@@ -130,6 +130,17 @@ def _stream(stream: Optional[torch.cuda.Stream]) -> int:
     return stream.cuda_stream
 
 
+def _made(stream: Optional[torch.cuda.Stream], make, *args, **kw) -> torch.Tensor:
+    """What a call allocates.  It belongs to the stream that the call runs on: a block of another stream's could be given to work
+    (or come from work) that does not wait for the call."""
+    if not stream:
+        return make(*args, **kw)
+    if not isinstance(stream, torch.cuda.Stream):     # any object that has a cuda_stream
+        stream = torch.cuda.ExternalStream(stream.cuda_stream)
+    with torch.cuda.stream(stream):
+        return make(*args, **kw)
+
+
 _Pose = C.c_float * 8
 
 
@@ -159,7 +170,8 @@ class WorldKV:
     """One library context plus the two device buffers it needs (allocated through torch).
 
     Method names and arguments mirror include/wk.h.  Tensors are CUDA tensors: bf16 [tokens, H, 128]
-    (or [tokens, D]) contiguous; index tensors int32.
+    (or [tokens, D]) contiguous; index tensors int32.  A call runs on ``stream``, or on the current one; what it
+    allocates belongs to that stream, as with ``torch.cuda.stream``.
     """
 
     def __init__(self, n_layers: int, n_heads: int, tokens_per_frame: int, n_keep: int, pool_slots: int, max_k: int,
@@ -210,7 +222,7 @@ class WorldKV:
             batch_stride_elems = K_chunks.stride(0) if K_chunks.dim() == 3 else self.F * self.T * self.D
         if keep_idx_out is None:
             shape = (batch, self.n_heads, self.C) if self.score_mode == SCORE_PER_HEAD else (batch, self.C)
-            keep_idx_out = torch.empty(shape, dtype=torch.int32, device=self.device)
+            keep_idx_out = _made(stream, torch.empty, shape, dtype=torch.int32, device=self.device)
         st = self.lib.wk_compress_chunk(self.ctx, K_chunks.data_ptr(), batch_stride_elems, batch,
                                         keep_idx_out.data_ptr(), _ptr(scores_out), _stream(stream))
         if st != WK_OK:
@@ -240,7 +252,7 @@ class WorldKV:
             batch_stride_elems = K_chunks.stride(0) if K_chunks.dim() == 3 else self.F * self.T * self.D
         if keep_idx is None:
             shape = (n, self.n_heads, self.C) if self.score_mode == SCORE_PER_HEAD else (n, self.C)
-            keep_idx = torch.empty(shape, dtype=torch.int32, device=self.device)
+            keep_idx = _made(stream, torch.empty, shape, dtype=torch.int32, device=self.device)
         pose_arr = _pose_arg(pose)
         slot_io, evicted = C.c_int32(slot), C.c_int32(-1)
         st = self.lib.wk_pool_compress_append(self.ctx, layer0, n, K_chunks.data_ptr(), V_chunks.data_ptr(),
@@ -270,7 +282,7 @@ class WorldKV:
                  dist_out: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, int]:
         """Returns (slots_out int32[max_k] on the device, count = min(k, M))."""
         if slots_out is None:
-            slots_out = torch.empty(max(1, self.max_k), dtype=torch.int32, device=self.device)
+            slots_out = _made(stream, torch.empty, max(1, self.max_k), dtype=torch.int32, device=self.device)
         pose_arr, n_out = _pose_arg(cur_pose), C.c_int32(0)
         st = self.lib.wk_retrieve(self.ctx, pose_arr, k, slots_out.data_ptr(), _ptr(dist_out), C.byref(n_out),
                                   _stream(stream))
@@ -306,9 +318,9 @@ class WorldKV:
                       scratch: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """Retrieval over a plain pose array [n, 8] fp32 of any length; returns ids_out int32 (-1 past the count)."""
         if ids_out is None:
-            ids_out = torch.empty(max(1, k), dtype=torch.int32, device=self.device)
+            ids_out = _made(stream, torch.empty, max(1, k), dtype=torch.int32, device=self.device)
         if scratch is None:
-            scratch = torch.empty(self.lib.wk_retrieve_scan_scratch_bytes(), dtype=torch.uint8, device=self.device)
+            scratch = _made(stream, torch.empty, self.lib.wk_retrieve_scan_scratch_bytes(), dtype=torch.uint8, device=self.device)
         pose_arr = _pose_arg(cur_pose)
         st = self.lib.wk_retrieve_scan(self.ctx, poses.data_ptr(), _ptr(valid), poses.shape[0], pose_arr, k,
                                        ids_out.data_ptr(), _ptr(dist_out), ids_out.numel(), scratch.data_ptr(),
@@ -321,7 +333,7 @@ class WorldKV:
                        score_out: Optional[torch.Tensor] = None, stream=None) -> Tuple[torch.Tensor, int]:
         """Query-based retrieval: returns (slots_out int32[max_k] on the device, count = min(k, M))."""
         if slots_out is None:
-            slots_out = torch.empty(max(1, self.max_k), dtype=torch.int32, device=self.device)
+            slots_out = _made(stream, torch.empty, max(1, self.max_k), dtype=torch.int32, device=self.device)
         n_out = C.c_int32(0)
         st = self.lib.wk_retrieve_query(self.ctx, layer, Q.data_ptr(), Q.shape[0], k, slots_out.data_ptr(), _ptr(score_out),
                                         C.byref(n_out), _stream(stream))
@@ -335,7 +347,7 @@ class WorldKV:
                          lse_out: Optional[torch.Tensor] = None, kv_splits: int = 0, stream=None) -> torch.Tensor:
         lq = Q.size(0)
         if O is None:
-            O = torch.empty_like(Q)
+            O = _made(stream, torch.empty_like, Q)
         n_segs = len(segs)
         arr = (wk_dense_seg * max(1, n_segs))()
         for i, (k, v) in enumerate(segs):

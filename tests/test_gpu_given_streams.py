@@ -63,6 +63,69 @@ def test_results_of_the_current_stream_are_as_before(kv, stream):
     torch.cuda.synchronize()
 
 
+def chunks(score_mode=0):
+    """The chunk pool's calls that allocate, as functions of a stream."""
+    from paper_2605_22718_b200 import WorldKV
+    T, H, F = 8, 2, 3
+    kv = WorldKV(n_layers=1, n_heads=H, tokens_per_frame=T, n_keep=4, pool_slots=4, max_k=700, max_lq=64, score_mode=score_mode)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    K, V = (torch.randn((1, F * T, H * 128), generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    poses = torch.randn((5000, 8), generator=g, device="cuda")
+    Q = torch.randn((40, H, 128), generator=g, device="cuda").to(torch.bfloat16)
+    pose = [0.0] * 8
+    slot, _, _ = kv.pool_compress_append(0, 1, K, V, pose)
+    seg = (K[0].view(-1, H, 128), V[0].view(-1, H, 128))
+    slots, scratch = gpu([slot]), torch.empty(kv.lib.wk_retrieve_scan_scratch_bytes(), dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    return kv, dict(
+        compress_chunk=lambda s: kv.compress_chunk(K, stream=s),
+        compress_append=lambda s: kv.pool_compress_append(0, 1, K, V, pose, evict_oldest_if_full=True, stream=s)[2],
+        retrieve=lambda s: kv.retrieve(pose, 1, stream=s)[0],
+        retrieve_scan=lambda s: kv.retrieve_scan(poses, pose, 20, scratch=scratch, stream=s),
+        retrieve_query=lambda s: kv.retrieve_query(0, Q, 1, stream=s)[0],
+        memory_attention=lambda s: kv.memory_attention(0, Q, [seg], slots, 1, stream=s))
+
+
+@pytest.mark.parametrize("what", ["compress_chunk", "compress_append", "retrieve", "retrieve_scan", "retrieve_query", "memory_attention"])
+def test_memory_of_the_chunk_pools_results_stays_with_its_stream(what):
+    kv, calls = chunks()
+    call, side = calls[what], torch.cuda.Stream()
+    x = call(side)
+    at, shape, dtype = x.data_ptr(), x.shape, x.dtype
+    del x
+    mine = [torch.empty(shape, dtype=dtype, device="cuda") for _ in range(4)]
+    assert at not in [m.data_ptr() for m in mine]
+    with torch.cuda.stream(side):
+        assert torch.empty(shape, dtype=dtype, device="cuda").data_ptr() == at
+    theirs = [m.data_ptr() for m in mine]
+    del mine
+    assert call(side).data_ptr() not in theirs
+    torch.cuda.synchronize()
+    for s in (None, 0, torch.cuda.current_stream()):
+        x = call(s)
+        at = x.data_ptr()
+        del x
+        assert torch.empty(shape, dtype=dtype, device="cuda").data_ptr() == at
+    torch.cuda.synchronize()
+
+
+def test_a_stream_object_of_another_kind():
+    """All that is asked of a stream is its handle."""
+    class Stream:
+        def __init__(self, s):
+            self.cuda_stream = s.cuda_stream
+    kv, calls = chunks()
+    want = calls["memory_attention"](None).clone()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = calls["memory_attention"](Stream(side))
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+    got = pages(kv)["O"](Stream(side))
+    torch.cuda.synchronize()
+    assert torch.isfinite(got).all()
+
+
 def test_steps_on_a_given_stream(kv):
     """Plan, store and attention on a stream of their own while the current one keeps allocating and overwriting blocks of the same
     sizes: the same results as one call after the other."""
