@@ -218,6 +218,15 @@ inline Divisor divisor(uint32_t d) {
   return {static_cast<uint32_t>(((1ull << (31 + l)) + d - 1) / d), 31 + l};
 }
 
+// The aligned word of four that byte i of an array of n lies in, and how many of its bytes the array has (the last word may be cut).
+struct ByteWord {
+  uint32_t at, bytes;
+};
+__host__ __device__ inline ByteWord word_of_byte(uint32_t i, uint32_t n) {
+  const uint32_t at = i & ~3u;
+  return {at, n - at < 4u ? n - at : 4u};
+}
+
 // Token-level cache in pages (entry points in wk_paged_api.cu).
 constexpr int kPlanMaxReq = 4096;   // four for each of 1,024 threads
 struct PlanArgs {

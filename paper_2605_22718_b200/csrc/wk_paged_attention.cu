@@ -51,6 +51,7 @@ struct Params {
   uint32_t page16, token16;        // strides in units of 16 bytes
   int64_t head_bytes;              // stride of a kv head
   int32_t counter_bytes;           // of the scratch buffer, before the pieces
+  uint32_t n_exps;                 // bytes of an array of exponents
   Divisor by_page, by_workers[2];  // by the warps that share a line: of one, of `lines`
 };
 
@@ -78,8 +79,8 @@ __device__ __forceinline__ void copy16(uint32_t dst, const void* src, uint32_t s
   asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %2, 0;\n\tcp.async.cg.shared.global [%0], [%1], 16, p;\n\t}"
                ::"r"(dst), "l"(src), "r"(skip) : "memory");
 }
-__device__ __forceinline__ void copy4(uint32_t dst, const void* src) {
-  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src, uint32_t bytes) {   // so many of the four are read
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
@@ -679,10 +680,11 @@ paged_attention(const __grid_constant__ Params p) {
         for (int k = 0; k < S::RL; ++k) {
           const uint32_t mask = __ballot_sync(0xffffffffu, row[k] != kNowhere);
           if (lane == 0) masks[warp][slot][k] = mask;
-          if constexpr (E4) {   // aligned words are what can be copied asynchronously: they hold the byte, and lie in the array's memory
+          if constexpr (E4) {   // aligned words are what can be copied asynchronously: the one with the byte, up to the array's end
             const uint32_t to_ex = ptx::smem_u32(exps) + slot * S::META + 8 * ((lane & (ST - 1)) + 32 * k);
-            copy4(to_ex, p.a.c.K_exp + (ex[k] & ~3u));
-            copy4(to_ex + 4, p.a.c.V_exp + (ex[k] & ~3u));
+            const ByteWord word = word_of_byte(ex[k], p.n_exps);
+            copy4(to_ex, p.a.c.K_exp + word.at, word.bytes);
+            copy4(to_ex + 4, p.a.c.V_exp + word.at, word.bytes);
             const uint32_t lo = __ballot_sync(0xffffffffu, ex[k] & 1), hi2 = __ballot_sync(0xffffffffu, ex[k] & 2);
             if (lane == 0) {
               masks[warp][slot][S::RL + 2 * k] = lo;
@@ -992,6 +994,7 @@ static wk_status launch_requests(wk_ctx* ctx, const PagedArgs& a, int32_t room, 
   p.page16 = static_cast<uint32_t>(a.c.page_stride * es / 16);
   p.token16 = static_cast<uint32_t>(a.c.token_stride * es / 16);
   p.head_bytes = a.c.head_stride * es;
+  p.n_exps = static_cast<uint32_t>(a.c.n_pages) * a.c.page_tokens * a.c.n_kv_heads;   // (8 bits: less than 2^32)
   p.by_page = divisor(a.c.page_tokens);
   using S = Shape<WK_BF16, 128, 1>;   // (all shapes have as many warps)
   p.by_workers[0] = divisor(ctx->sm_count * S::W);
