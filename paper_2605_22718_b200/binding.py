@@ -446,6 +446,8 @@ class PagedKV:
     def page_store(self, K_new: torch.Tensor, V_new: torch.Tensor, slots: torch.Tensor, stream=None) -> None:
         """Rows K_new, V_new [n, n_kv_heads, head_dim] (heads contiguous, any row stride, both alike) into slots [>= n]."""
         kv = self.kv
+        if self._desc is None:
+            raise WkError(WK_ERR_ARG, "page_store: a cache that only plans (made without K and V)")
         r = self._native.page_store(kv.ctx.value if kv.ctx else 0, self._index, self._desc_at, K_new, V_new, slots,
                                     stream.cuda_stream if stream else None)
         if r is not None:
@@ -458,6 +460,8 @@ class PagedKV:
         row stride) over the tokens that tables and lens name.  scratch: as WorldKV's, shared by the calls of a context unless
         given (zero-filled once; for calls that may overlap on the GPU)."""
         kv = self.kv
+        if self._desc is None:
+            raise WkError(WK_ERR_ARG, "paged_attention: a cache that only plans (made without K and V)")
         r = self._native.paged_attention(kv.ctx.value if kv.ctx else 0, self._index, self._desc_at, Q, tables, lens, window, sink,
                                          softmax_scale, O, lse_out, scratch if scratch is not None else kv.paged_scratch,
                                          stream.cuda_stream if stream else None)
