@@ -84,6 +84,13 @@ at::Tensor empty(at::IntArrayRef sizes, const at::Tensor& x, const Arguments& a)
   return at::Tensor(at::detail::empty_cuda(sizes, x.scalar_type(), x.device(), std::nullopt));
 }
 PyObject* said(const char* what) { return PyUnicode_FromString(what); }
+PyObject* pair_of(const at::Tensor& x, const at::Tensor& y) {
+  PyObject* pair = PyTuple_New(2);
+  if (!pair) return nullptr;
+  PyTuple_SET_ITEM(pair, 0, THPVariable_Wrap(x));
+  PyTuple_SET_ITEM(pair, 1, THPVariable_Wrap(y));
+  return pair;
+}
 
 // The library's calls wait where the GPU's queue is full: other Python threads run meanwhile.
 template <typename F>
@@ -126,17 +133,22 @@ PyObject* page_plan(PyObject*, PyObject* const* args, Py_ssize_t n_args) {
   if (PyErr_Occurred()) return nullptr;
   const at::Tensor slots = slots_in ? *slots_in : empty({max_tokens}, *lens, a);
   const at::Tensor starts = starts_in ? *starts_in : empty({n + 1}, *lens, a);
+  if (n == 0) {   // nothing to plan: no rows, and the ring as it is
+    if (n_pages < 1 || page_tokens < 1) return PyLong_FromLong(WK_ERR_ARG);
+    c10::cuda::OptionalCUDAStreamGuard guard;
+    if (a.given) guard.reset_stream(*a.given);
+    slots.view(-1).narrow(0, 0, max_tokens).fill_(-1);
+    starts.view(-1).narrow(0, 0, 1).zero_();
+    if (state_out && !state_out->is_same(*state)) state_out->view(-1).narrow(0, 0, 4).copy_(state->view(-1).narrow(0, 0, 4));
+    return pair_of(slots, starts);
+  }
   const wk_status st = without_lock([&] { return call_plan(
       ctx, n_pages, page_tokens, static_cast<int32_t>(n), lens->data_ptr<int32_t>(), more->data_ptr<int32_t>(),
       (lens_out ? lens_out : lens)->data_ptr<int32_t>(), tables->data_ptr<int32_t>(), static_cast<int32_t>(tables->size(1)),
       tables->stride(0), ring->data_ptr<int32_t>(), state->data_ptr<int32_t>(), (state_out ? state_out : state)->data_ptr<int32_t>(),
       max_tokens, slots.data_ptr<int32_t>(), starts.data_ptr<int32_t>(), stream); });
   if (st != WK_OK) return PyLong_FromLong(st);
-  PyObject* pair = PyTuple_New(2);
-  if (!pair) return nullptr;
-  PyTuple_SET_ITEM(pair, 0, THPVariable_Wrap(slots));
-  PyTuple_SET_ITEM(pair, 1, THPVariable_Wrap(starts));
-  return pair;
+  return pair_of(slots, starts);
   END_HANDLE_TH_ERRORS
 }
 
