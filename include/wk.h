@@ -292,6 +292,8 @@ typedef struct {
  *   new_tokens[r] < 0   the request ends: its pages go to the back of the ring (for the next call), its length becomes 0; its
  *                       table row stays as it is.  Entries outside 0 .. n_pages - 1 are left out (other than -1: WK_DEV_BAD_SLOT)
  *   lens[r] < 0         no request: takes no part (with new_tokens[r] > 0 it is refused)
+ *                       Pages have one owner: those of an ended request go back even where another table lists them, and
+ *                       will be given out while that one still uses them
  *   lens_out [n_req]    the lengths afterwards; may be lens
  *   tables [n_req]      rows of max_pages int32, table_stride apart; only new entries are written
  *   ring [n_pages]      page ids; the free ones are ring[(head + i) mod n_pages], i < count
@@ -302,7 +304,8 @@ typedef struct {
  *   slots_out [max_tokens]   slot (page * page_tokens + place in the page) of every new token, request after request; -1 for the
  *                       rows of refused requests, for tokens whose page id is out of range (WK_DEV_BAD_SLOT), and past the last row
  *   starts_out [n_req + 1]   first row of every request, then the number of rows (int32, saturating)
- * Errors: WK_ERR_SHAPE (n_req > 4096, n_req * max_pages or n_pages * page_tokens >= 2^31), WK_ERR_ARG. */
+ * Errors: WK_ERR_SHAPE (n_req > 4096, n_req * max_pages or n_pages * page_tokens >= 2^31), WK_ERR_ARG (n_req < 1 among them: with no
+ * request there is nothing to plan). */
 wk_status wk_page_plan(wk_ctx* ctx, int32_t n_pages, int32_t page_tokens, int32_t n_req, const int32_t* lens,
                        const int32_t* new_tokens, int32_t* lens_out, int32_t* tables, int32_t max_pages,
                        int64_t table_stride, int32_t* ring, int32_t* state, int32_t* state_out, int32_t max_tokens,
@@ -320,7 +323,9 @@ wk_status wk_page_store(wk_ctx* ctx, const wk_paged_kv* cache, const void* K_new
                         int32_t n_tokens, int64_t row_stride, const int32_t* slots, void* stream);
 
 /* Scratch of wk_paged_attention: partial results of requests that several CTAs share, and their counters.  Zero-filled by the
- * caller the first time; every call leaves the counters zero.  Calls that share it must not overlap on the GPU. */
+ * caller the first time; every call leaves the counters zero.  Calls that share it must not overlap on the GPU (captured ones, on
+ * whichever graph's replay, included): the results of such calls are undefined, and so are those of later calls, unreported, until the
+ * caller has zero-filled the scratch again. */
 size_t wk_paged_scratch_bytes(const wk_ctx* ctx);
 
 /* Attention of one new token per request: for request r and head h, with kv head h / (n_heads / n_kv_heads),
@@ -335,6 +340,9 @@ size_t wk_paged_scratch_bytes(const wk_ctx* ctx);
  *   lens [n_req]  0: nothing is attended, O = 0 and lse = -inf; negative: the request's rows of O and lse_out stay as they are
  *   lse_out [n_req][n_heads] fp32 (natural log) or NULL.  A row in which no key has any weight (none visible, all logits
  *             -inf) is O = 0, lse = -inf; a logit that is NaN or +inf makes its row NaN
+ * Logits and sums are fp32.  A weight meets V rounded to the cache's type, in 8 bits (times its row's power of two) to fp16: in fp16 it is
+ * off by 2^-32 of the row's largest where that is more, so below 2^-33 of it it is zero.  A visible value that is not finite makes its
+ * column of O infinite or NaN: NaN where its weight is rounded to zero.
  *   softmax_scale 0 selects 1/sqrt(head_dim); window 0: all tokens
  *   scratch   wk_paged_scratch_bytes() bytes, 256-byte aligned
  * Errors: WK_ERR_SHAPE (n_heads not a multiple of n_kv_heads, scratch too small), WK_ERR_ARG. */

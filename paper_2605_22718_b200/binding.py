@@ -458,7 +458,9 @@ class PagedKV:
                         scratch: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
         """O [n_req, n_heads, head_dim] of one new token per request: Q [n_req, n_heads, head_dim] (heads contiguous, any
         row stride) over the tokens that tables and lens name.  scratch: as WorldKV's, shared by the calls of a context unless
-        given (zero-filled once; for calls that may overlap on the GPU)."""
+        given.  Calls that may overlap on the GPU (on several streams, or replayed from several graphs) need one each, zero-filled once:
+        where two have overlapped on one, all later results on it are undefined until it is zero-filled again
+        (``kv.paged_scratch.zero_()``)."""
         kv = self.kv
         if self._desc is None:
             raise WkError(WK_ERR_ARG, "paged_attention: a cache that only plans (made without K and V)")
