@@ -342,7 +342,8 @@ size_t wk_paged_scratch_bytes(const wk_ctx* ctx);
  *             -inf) is O = 0, lse = -inf; a logit that is NaN or +inf makes its row NaN
  * Logits and sums are fp32.  A weight meets V rounded to the cache's type, in 8 bits (times its row's power of two) to fp16: in fp16 it is
  * off by 2^-32 of the row's largest where that is more, so below 2^-33 of it it is zero.  A visible value that is not finite makes its
- * column of O infinite or NaN: NaN where its weight is rounded to zero.
+ * column of O infinite or NaN: NaN where its weight is rounded to zero.  Sums of up to 2^8 |V| over the tokens have to stay in fp32's
+ * range: in bf16 they do at any length for values below 2^88.
  *   softmax_scale 0 selects 1/sqrt(head_dim); window 0: all tokens
  *   scratch   wk_paged_scratch_bytes() bytes, 256-byte aligned
  * Errors: WK_ERR_SHAPE (n_heads not a multiple of n_kv_heads, scratch too small), WK_ERR_ARG. */

@@ -20,7 +20,8 @@
 //     log2), which one vote per step finds out, so weights reach at most 2^8; sums are fp32.  Weights are rounded to the type of V
 //     for the second product (bf16 or fp16, half a step 2^-8 or 2^-11 of the weight; the normalising sum is of the unrounded ones).
 //     fp16 has steps of 2^-24 at its lower end, and a long tail of small weights may add up to all that a row has: there the
-//     weights are taken 2^7 times as large (at most 2^15), so that one is off by 2^-32 of the largest at most.
+//     weights are taken 2^7 times as large (at most 2^15), so that one is off by 2^-32 of the largest at most.  Exponentials,
+//     logarithms and quotients are the SM's approximations (2^-22 or so of the value, 2^-21 of a logarithm): small beside that.
 //   * 8 bits.  Codes are exact in fp16.  A key's power of two joins the logit's scale, a value's is added to the logit that its
 //     weight is taken from (with a reference of its own), so that both products have fp16 operands of ordinary size; Q is brought
 //     into fp16 by a power of two per row, exactly.
@@ -57,8 +58,8 @@ struct Params {
 
 template <int MODE, int D, int NT>
 struct Shape {
-  // As many warps as keep the memory busy, and no more: with fewer copies in flight the SMs are served more evenly (1.35 GB in
-  // bf16: 6 warps 230 us, 7 207, 8 204, 10 211; with a third step in the ring 218.  0.92 GB in 8 bits: 7 170, 8 174, 10 188).
+  // As measured, warps x steps in a warp's ring (us for 1.35 GB in bf16 / 0.92 GB in 8 bits): 6 x 2 210 / 187, 7 x 2 207 / 172, 8 x 2
+  // 207 / 165, 9 x 2 214 / 177, 10 x 2 216 / 168, 6 x 3 212 / 188, 7 x 3 221 / 175 (8 x 3 has no room).
   static constexpr int W = 8;
   static constexpr int STAGES = 2;
   static constexpr int ES = MODE == WK_E4M3 ? 1 : 2;     // bytes per element of the cache

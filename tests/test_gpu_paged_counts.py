@@ -111,6 +111,7 @@ CASES = [
     ("f16", 64, 32, 8, [55] * 20, 0, 0), ("e4m3", 64, 8, 8, [205] * 31, 0, 0), ("bf16", 128, 4, 1, [120, 136, 8] * 20, 0, 0),
     ("bf16", 64, 20, 1, [90] * 16, 0, 0), ("bf16", 128, 28, 4, [500 + 997 * i % 20000 for i in range(24)], 1760, 880),
     ("f16", 128, 3, 3, [-1, 40, 0, 17, -1] * 12 + [-1] * 50, 0, 0), ("e4m3", 128, 16, 16, [256, 257, 31] * 11, 0, 0),
+    ("f16", 64, 2, 1, [13 * i % 40 - 1 for i in range(9000)], 0, 0),
     ("f16", 128, 9, 1, [3000], 16, 0), ("e4m3", 64, 4, 4, [0, 1, 2, 63, 64, 65, 127, 128, 129], 0, 0),
 ]
 
