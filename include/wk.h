@@ -290,10 +290,10 @@ typedef struct {
  *                       ask for are more than are free (one that needs no new page is not refused for that):
  *                       WK_DEV_POOL_FULL is set
  *   new_tokens[r] < 0   the request ends: its pages go to the back of the ring (for the next call), its length becomes 0; its
- *                       table row stays as it is.  Entries outside 0 .. n_pages - 1 are left out (other than -1: WK_DEV_BAD_SLOT)
+ *                       table row stays as it is.  Entries outside 0 .. n_pages - 1 are left out (other than -1: WK_DEV_BAD_SLOT).
+ *                       A page has one owner: it goes back even where another table lists it, and will be given out while
+ *                       that one still uses it
  *   lens[r] < 0         no request: takes no part (with new_tokens[r] > 0 it is refused)
- *                       Pages have one owner: those of an ended request go back even where another table lists them, and
- *                       will be given out while that one still uses them
  *   lens_out [n_req]    the lengths afterwards; may be lens
  *   tables [n_req]      rows of max_pages int32, table_stride apart; only new entries are written
  *   ring [n_pages]      page ids; the free ones are ring[(head + i) mod n_pages], i < count
@@ -341,7 +341,7 @@ size_t wk_paged_scratch_bytes(const wk_ctx* ctx);
  *   lse_out [n_req][n_heads] fp32 (natural log) or NULL.  A row in which no key has any weight (none visible, all logits
  *             -inf) is O = 0, lse = -inf; a logit that is NaN or +inf makes its row NaN
  * Logits and sums are fp32.  A weight meets V rounded to the cache's type, in 8 bits (times its row's power of two) to fp16: in fp16 it is
- * off by 2^-32 of the row's largest where that is more, so below 2^-33 of it it is zero.  A visible value that is not finite makes its
+ * off by 2^-32 of the row's largest where that is more, and zero below 2^-33 of that.  A visible value that is not finite makes its
  * column of O infinite or NaN: NaN where its weight is rounded to zero.  Sums of up to 2^8 |V| over the tokens have to stay in fp32's
  * range: in bf16 they do at any length for values below 2^88.
  *   softmax_scale 0 selects 1/sqrt(head_dim); window 0: all tokens
